@@ -1,4 +1,5 @@
-"""ctypes binding of the C ABI in include/vpp_chunk_attn.h (argument marshalling only).
+"""ctypes binding of the C ABI in include/vpp_chunk_attn.h, vpp_rope.h and vpp_block_attn.h
+(argument marshalling only).
 
 Every function here has the name of the C entry point it calls. All the work of
 the path runs in the HIP library; if that library is missing this module raises
@@ -27,6 +28,13 @@ EXPORTED = [
     "vpp_status_str", "vpp_chunk_attn_plan_info", "vpp_chunk_attn_plan_items",
     "vpp_chunk_attn_run_paged", "vpp_kv_append_paged", "vpp_paged_slot_mapping",
     "vpp_chunk_attn_run_mla", "vpp_chunk_attn_run_noalloc",
+]
+
+# the entry points of vpp_rope.h and of vpp_block_attn.h
+EXPORTED_ROPE = ["vpp_rope_turns", "vpp_rope", "vpp_rope_append_paged"]
+EXPORTED_BLOCK = [
+    "vpp_query_blocks", "vpp_completed_blocks", "vpp_block_summarize_paged", "vpp_block_select_paged",
+    "vpp_block_attn_workspace", "vpp_block_attn_run_paged",
 ]
 
 # bytes of the static device scratch behind vpp_chunk_attn_run_noalloc
@@ -67,6 +75,34 @@ class PlanInfo(ctypes.Structure):
         ("num_slots", ctypes.c_int32),
     ]
 
+
+class RopeConfig(ctypes.Structure):
+    _fields_ = [
+        ("head_dim", ctypes.c_int32),
+        ("rotary_dim", ctypes.c_int32),
+        ("offset", ctypes.c_int32),
+        ("interleaved", ctypes.c_int32),
+        ("scale", ctypes.c_float),
+    ]
+
+
+class BlockConfig(ctypes.Structure):
+    _fields_ = [
+        ("num_q_heads", ctypes.c_int32),
+        ("num_kv_heads", ctypes.c_int32),
+        ("head_dim_qk", ctypes.c_int32),
+        ("head_dim_v", ctypes.c_int32),
+        ("softmax_scale", ctypes.c_float),
+        ("block_size", ctypes.c_int32),
+        ("query_block", ctypes.c_int32),
+        ("max_blocks", ctypes.c_int32),
+        ("sink_blocks", ctypes.c_int32),
+        ("local_blocks", ctypes.c_int32),
+    ]
+
+
+QUERY_BLOCK_DTYPE = np.dtype([("row0", "<i4"), ("rows", "<i4"), ("segment", "<i4"), ("pos0", "<i4"),
+                              ("kv_start", "<i4"), ("reserved", "<i4", (3,))])
 
 WORK_ITEM_DTYPE = np.dtype([("row0", "<i4"), ("nrows", "<i4"), ("pos0", "<i4"),
                             ("key_begin", "<i4"), ("key_end", "<i4"), ("split", "<i4"),
@@ -114,6 +150,22 @@ def load(path: Optional[str] = None):
                                         i32, i32, i32, i32, i32, i32, vp, vp]
     lib.vpp_paged_slot_mapping.restype = ctypes.c_int
     lib.vpp_paged_slot_mapping.argtypes = [i32, vp, vp, vp, vp, i64, i32, i32, vp]
+    lib.vpp_rope_turns.argtypes = [i32, vp, vp]
+    lib.vpp_rope.argtypes = [ctypes.POINTER(RopeConfig), vp, i64, i64, vp, i64, i64, i32, i32, vp, vp, i32, vp]
+    lib.vpp_rope_append_paged.argtypes = [ctypes.POINTER(RopeConfig), vp, i64, i64, vp, i64, i64, vp, i64, i64,
+                                          vp, i64, i64, vp, i64, i64, i64, vp, i64, i64, i64,
+                                          i32, i32, i32, i32, i32, i32, vp, vp, vp, vp]
+    blk = ctypes.POINTER(BlockConfig)
+    count = ctypes.POINTER(i32)
+    lib.vpp_query_blocks.argtypes = [i32, vp, vp, vp, i32, i32, vp, i32, count]
+    lib.vpp_completed_blocks.argtypes = [i32, vp, vp, vp, vp, i64, i32, i32, i32, vp, i32, count]
+    lib.vpp_block_summarize_paged.argtypes = [blk, vp, i64, i64, i64, i32, i32, vp, i32, vp, vp]
+    lib.vpp_block_select_paged.argtypes = [blk, vp, i32, vp, i64, i64, i32, vp, i32, i32, vp, i64, i32, i32, i64, vp, vp]
+    lib.vpp_block_attn_workspace.argtypes = [blk, i32, i32, ctypes.POINTER(sz)]
+    lib.vpp_block_attn_run_paged.argtypes = [blk, vp, i32, vp, i64, i64, i32, vp, i64, i64, i64, vp, i64, i64, i64,
+                                             i32, i32, vp, i64, i32, i32, vp, vp, i64, i64, vp, i64, vp, sz, vp]
+    for name in EXPORTED_ROPE + EXPORTED_BLOCK:
+        getattr(lib, name).restype = ctypes.c_int
     if path == LIB_PATH:
         _lib = lib
     return lib
@@ -140,6 +192,9 @@ def load_torch():
         ext.bind(*(ctypes.cast(fn, ctypes.c_void_p).value
                    for fn in (lib.vpp_chunk_attn_run, lib.vpp_chunk_attn_run_noalloc, lib.vpp_chunk_attn_run_mla,
                               lib.vpp_chunk_attn_run_paged, lib.vpp_kv_append_paged)))
+        ext.bind_sparse(*(ctypes.cast(fn, ctypes.c_void_p).value
+                          for fn in (lib.vpp_rope, lib.vpp_rope_append_paged, lib.vpp_block_summarize_paged,
+                                     lib.vpp_block_select_paged, lib.vpp_block_attn_run_paged)))
         _torch_ext = ext
     return _torch_ext
 
@@ -245,6 +300,103 @@ def vpp_paged_slot_mapping(cu_q: Sequence[int], kv_start: Sequence[int], prefix_
     if st != VPP_OK:
         raise VppError(st, "vpp_paged_slot_mapping")
     return out
+
+
+def _call(name: str, *args) -> None:
+    st = getattr(load(), name)(*args)
+    if st != VPP_OK:
+        raise VppError(st, name)
+
+
+def vpp_rope_turns(frequency: Sequence[float]) -> np.ndarray:
+    """Angles per position in turns (uint64 fixed point) of the frequencies in radians, one for
+    each pair of rotated dims."""
+    f = _arr(frequency, np.float64)
+    out = np.zeros(len(f), dtype=np.uint64)
+    _call("vpp_rope_turns", 2 * len(f), f.ctypes.data, out.ctypes.data)
+    return out
+
+
+def vpp_rope(cfg: RopeConfig, x_ptr: int, x_st: int, x_sh: int, out_ptr: int, o_st: int, o_sh: int,
+             num_tokens: int, num_heads: int, turns_ptr: int, positions_ptr: int, inverse: int, stream: int) -> None:
+    _call("vpp_rope", ctypes.byref(cfg), x_ptr, x_st, x_sh, out_ptr, o_st, o_sh, num_tokens, num_heads,
+          turns_ptr, positions_ptr, inverse, stream)
+
+
+def vpp_rope_append_paged(cfg: RopeConfig, q_ptr: int, q_st: int, q_sh: int, qo_ptr: int, qo_st: int, qo_sh: int,
+                          kn_ptr: int, kn_st: int, kn_sh: int, vn_ptr: int, vn_st: int, vn_sh: int,
+                          k_ptr: int, k_sp: int, k_st: int, k_sh: int, v_ptr: int, v_sp: int, v_st: int, v_sh: int,
+                          num_tokens: int, num_q_heads: int, num_kv_heads: int, dv: int, page_size: int,
+                          num_pages: int, turns_ptr: int, positions_ptr: int, slots_ptr: int, stream: int) -> None:
+    _call("vpp_rope_append_paged", ctypes.byref(cfg), q_ptr, q_st, q_sh, qo_ptr, qo_st, qo_sh, kn_ptr, kn_st, kn_sh,
+          vn_ptr, vn_st, vn_sh, k_ptr, k_sp, k_st, k_sh, v_ptr, v_sp, v_st, v_sh, num_tokens, num_q_heads,
+          num_kv_heads, dv, page_size, num_pages, turns_ptr, positions_ptr, slots_ptr, stream)
+
+
+def _segments(cu_q, kv_start, prefix_len):
+    cu, ks, pl = _arr(cu_q, np.int32), _arr(kv_start, np.int64), _arr(prefix_len, np.int64)
+    if len(cu) != len(ks) + 1 or len(pl) != len(ks):
+        raise ValueError("cu_q must have one more entry than kv_start and prefix_len")
+    return cu, ks, pl
+
+
+def vpp_query_blocks(cu_q: Sequence[int], kv_start: Sequence[int], prefix_len: Sequence[int], query_block: int,
+                     block_size: int) -> np.ndarray:
+    """The query blocks of a chunk (array of QUERY_BLOCK_DTYPE, in row order)."""
+    cu, ks, pl = _segments(cu_q, kv_start, prefix_len)
+    most = int(cu[-1]) // max(1, int(query_block)) + len(ks) if len(cu) else 0  # a short one a segment
+    out = np.zeros(max(0, most), dtype=QUERY_BLOCK_DTYPE)
+    n = ctypes.c_int32(0)
+    _call("vpp_query_blocks", len(ks), cu.ctypes.data, ks.ctypes.data, pl.ctypes.data, query_block, block_size,
+          out.ctypes.data, len(out), ctypes.byref(n))
+    return out[:n.value]
+
+
+def vpp_completed_blocks(cu_q: Sequence[int], kv_start: Sequence[int], prefix_len: Sequence[int],
+                         block_table: np.ndarray, page_size: int, block_size: int) -> np.ndarray:
+    """Indices (int64) of the blocks of the cache that the chunk completes; block_table is a host int32
+    [segments, pages_per_row] array."""
+    cu, ks, pl = _segments(cu_q, kv_start, prefix_len)
+    bt = _arr(block_table, np.int32)
+    if bt.ndim != 2 or bt.shape[0] < len(ks):
+        raise ValueError("segment metadata and block table do not match")
+    most = int(cu[-1]) // max(1, int(block_size)) + len(ks) if len(cu) else 0  # one that a segment only ends
+    out = np.zeros(max(0, most), dtype=np.int64)
+    n = ctypes.c_int32(0)
+    _call("vpp_completed_blocks", len(ks), cu.ctypes.data, ks.ctypes.data, pl.ctypes.data, bt.ctypes.data,
+          bt.shape[1], bt.shape[1], page_size, block_size, out.ctypes.data, len(out), ctypes.byref(n))
+    return out[:n.value]
+
+
+def vpp_block_summarize_paged(cfg: BlockConfig, k_ptr: int, k_sp: int, k_st: int, k_sh: int, page_size: int,
+                              num_pages: int, blocks_ptr: int, num_blocks: int, summaries_ptr: int, stream: int) -> None:
+    _call("vpp_block_summarize_paged", ctypes.byref(cfg), k_ptr, k_sp, k_st, k_sh, page_size, num_pages, blocks_ptr,
+          num_blocks, summaries_ptr, stream)
+
+
+def vpp_block_select_paged(cfg: BlockConfig, qb_ptr: int, num_query_blocks: int, q_ptr: int, q_st: int, q_sh: int,
+                           num_tokens: int, summaries_ptr: int, page_size: int, num_pages: int, bt_ptr: int,
+                           bt_st: int, num_segments: int, pages_per_row: int, max_kv_len: int, blocks_ptr: int,
+                           stream: int) -> None:
+    _call("vpp_block_select_paged", ctypes.byref(cfg), qb_ptr, num_query_blocks, q_ptr, q_st, q_sh, num_tokens,
+          summaries_ptr, page_size, num_pages, bt_ptr, bt_st, num_segments, pages_per_row, max_kv_len, blocks_ptr,
+          stream)
+
+
+def vpp_block_attn_workspace(cfg: BlockConfig, num_query_blocks: int, num_tokens: int) -> int:
+    n = ctypes.c_size_t(0)
+    _call("vpp_block_attn_workspace", ctypes.byref(cfg), num_query_blocks, num_tokens, ctypes.byref(n))
+    return n.value
+
+
+def vpp_block_attn_run_paged(cfg: BlockConfig, qb_ptr: int, num_query_blocks: int, q_ptr: int, q_st: int, q_sh: int,
+                             num_tokens: int, k_ptr: int, k_sp: int, k_st: int, k_sh: int, v_ptr: int, v_sp: int,
+                             v_st: int, v_sh: int, page_size: int, num_pages: int, bt_ptr: int, bt_st: int,
+                             num_segments: int, pages_per_row: int, blocks_ptr: int, out_ptr: int, o_st: int,
+                             o_sh: int, lse_ptr: int, lse_sh: int, ws_ptr: int, ws_bytes: int, stream: int) -> None:
+    _call("vpp_block_attn_run_paged", ctypes.byref(cfg), qb_ptr, num_query_blocks, q_ptr, q_st, q_sh, num_tokens,
+          k_ptr, k_sp, k_st, k_sh, v_ptr, v_sp, v_st, v_sh, page_size, num_pages, bt_ptr, bt_st, num_segments,
+          pages_per_row, blocks_ptr, out_ptr, o_st, o_sh, lse_ptr, lse_sh, ws_ptr, ws_bytes, stream)
 
 
 def vpp_chunk_attn_destroy(plan: Optional[int]) -> None:

@@ -1,5 +1,5 @@
-"""Build the native libraries in-tree: the HIP attention library (hipcc for gfx950) into
-paper_2608_26523_amd/libvpp_chunk_attn.so, the host-only schedule model (g++) into
+"""Build the native libraries in-tree: the HIP library (hipcc for gfx950: chunk attention, rotary
+positions, block-sparse attention) into paper_2608_26523_amd/libvpp_chunk_attn.so, the host-only schedule model (g++) into
 paper_2608_26523_amd/libvpp_sched.so, and the extension that calls the attention library on
 torch tensors (g++) into paper_2608_26523_amd/vpp_torch.so."""
 from __future__ import annotations
@@ -11,6 +11,7 @@ import sys
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 SRC = os.path.join(PKG, "csrc", "vpp_chunk_attn.hip")
+MORE_SRCS = [os.path.join(PKG, "csrc", name) for name in ("vpp_rope.hip", "vpp_block_attn.hip")]
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "libvpp_chunk_attn.so")
 SCHED_SRC = os.path.join(PKG, "csrc", "vpp_sched.cpp")
@@ -35,13 +36,15 @@ PARTS = (0, 1, 2)  # VPP_PART values: host code + contiguous-cache kernels, page
 
 
 def build(extra_flags=(), out: str = LIB, quiet: bool = True, src: str = None) -> str:
-    """Compile the parts of the HIP source in parallel (one hipcc each), then link."""
+    """Compile the parts of the attention source and the other HIP sources in parallel (one hipcc
+    each), then link."""
     src = src or SRC
     base = [hipcc()] + HIPCC_FLAGS + list(extra_flags) + ["-I", INCLUDE]
-    objs = [out + ".part%d.o" % part for part in PARTS]
+    units = [(src, ["-DVPP_PART=%d" % part]) for part in PARTS] + [(more, []) for more in MORE_SRCS]
+    objs = [out + ".part%d.o" % i for i in range(len(units))]
     procs = []
-    for part, obj in zip(PARTS, objs):
-        cmd = [c for c in base if c != "-shared"] + ["-c", "-DVPP_PART=%d" % part, "-o", obj, src]
+    for (unit, defines), obj in zip(units, objs):
+        cmd = [c for c in base if c != "-shared"] + ["-c"] + defines + ["-o", obj, unit]
         procs.append(subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True))
     outs = [pr.communicate()[0] for pr in procs]
     msgs = [ln for o in outs for ln in o.splitlines() if "packed-fp32-ops" not in ln and ln.strip()]

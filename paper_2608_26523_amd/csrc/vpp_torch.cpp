@@ -14,7 +14,13 @@
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <ATen/ops/empty.h>
+
+#include <cstring>
+
+#include "vpp_block_attn.h"
 #include "vpp_chunk_attn.h"
+#include "vpp_rope.h"
 
 namespace {
 
@@ -27,6 +33,11 @@ struct Api {
     decltype(&vpp_chunk_attn_run_mla) run_mla = nullptr;
     decltype(&vpp_chunk_attn_run_paged) run_paged = nullptr;
     decltype(&vpp_kv_append_paged) append = nullptr;
+    decltype(&vpp_rope) rope = nullptr;
+    decltype(&vpp_rope_append_paged) rope_append = nullptr;
+    decltype(&vpp_block_summarize_paged) block_summarize = nullptr;
+    decltype(&vpp_block_select_paged) block_select = nullptr;
+    decltype(&vpp_block_attn_run_paged) block_run = nullptr;
 } api;
 
 // A tensor argument: torch's own class, a plain strided GPU tensor of the given
@@ -265,6 +276,267 @@ int caller_init(PyObject* self, PyObject* args, PyObject*) {
     return 0;
 }
 
+// ---------------------------------------------------------------------------------------------
+// rotary positions
+// ---------------------------------------------------------------------------------------------
+struct Rope {
+    PyObject_HEAD
+    vpp_rope_config_t cfg;
+    const uint64_t* turns;
+    int device;
+};
+
+bool fits32(std::initializer_list<int64_t> sizes) {
+    for (const int64_t x : sizes)
+        if (x > INT32_MAX) return false;
+    return true;
+}
+
+// rotate(x, positions, out, inverse)
+PyObject* rope_rotate(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+    const Rope* c = (Rope*)self;
+    View x, out, pos;
+    int64_t tokens = 0, heads = 0;
+    int inverse = 0;
+    void* stream = nullptr;
+    return checked_call(
+        [&] {
+            if (n != 4 || !PyBool_Check(a[3])) return false;
+            const at::Tensor *tx = plain(a[0], c->device, at::kBFloat16, 3), *to = plain(a[2], c->device, at::kBFloat16, 3);
+            const at::Tensor* tp = plain(a[1], c->device, at::kLong, 1);
+            if (!tx || !to || !tp || (int)c10::hip::current_device() != c->device) return false;
+            tokens = tx->size(0), heads = tx->size(1);
+            if (tokens < 1 || heads < 1 || !fits32({tokens, heads})) return false;
+            if (tx->size(2) != c->cfg.head_dim || to->sizes() != tx->sizes() || tp->size(0) != tokens) return false;
+            x = View(tx), out = View(to), pos = View(tp);
+            inverse = a[3] == Py_True;
+            stream = stream_of(c->device);
+            return true;
+        },
+        [&] {
+            return api.rope(&c->cfg, x.p, x.s0, x.s1, out.p, out.s0, out.s1, (int32_t)tokens, (int32_t)heads, c->turns,
+                            (const int64_t*)pos.p, inverse, stream);
+        });
+}
+
+// append(q or None, k_new, v_new, k_pages, v_pages, slot_mapping, positions, q_out or None)
+PyObject* rope_append(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+    const Rope* c = (Rope*)self;
+    View q, qo, kn, vn, k, v, slots, pos;
+    int64_t tokens = 0, hq = 0, heads = 0, dv = 0, pages = 0, page = 0;
+    void* stream = nullptr;
+    return checked_call(
+        [&] {
+            if (n != 8 || (a[0] == Py_None) != (a[7] == Py_None)) return false;
+            const int dev = c->device;
+            const at::Tensor *tkn = plain(a[1], dev, at::kBFloat16, 3), *tvn = plain(a[2], dev, at::kBFloat16, 3);
+            const at::Tensor *tk = plain(a[3], dev, at::kBFloat16, 4), *tv = plain(a[4], dev, at::kBFloat16, 4);
+            const at::Tensor *ts = plain(a[5], dev, at::kLong, 1), *tp = plain(a[6], dev, at::kLong, 1);
+            if (!tkn || !tvn || !tk || !tv || !ts || !tp || (int)c10::hip::current_device() != dev) return false;
+            tokens = tkn->size(0), heads = tkn->size(1), dv = tvn->size(2), pages = tk->size(0), page = tk->size(1);
+            if (tokens < 1 || heads < 1 || !fits32({tokens, heads, dv, pages, page})) return false;
+            const int64_t d = c->cfg.head_dim;
+            if (tkn->size(2) != d || tvn->size(0) != tokens || tvn->size(1) != heads) return false;
+            if (tk->size(2) != heads || tk->size(3) != d || tv->size(0) != pages || tv->size(1) != page ||
+                tv->size(2) != heads || tv->size(3) != dv || ts->size(0) != tokens || tp->size(0) != tokens)
+                return false;
+            if (a[0] != Py_None) {
+                const at::Tensor *tq = plain(a[0], dev, at::kBFloat16, 3), *to = plain(a[7], dev, at::kBFloat16, 3);
+                if (!tq || !to || tq->size(0) != tokens || tq->size(2) != d || to->sizes() != tq->sizes()) return false;
+                hq = tq->size(1);
+                if (hq < 1 || !fits32({hq})) return false;
+                q = View(tq), qo = View(to);
+            }
+            kn = View(tkn), vn = View(tvn), k = View(tk), v = View(tv), slots = View(ts), pos = View(tp);
+            stream = stream_of(dev);
+            return true;
+        },
+        [&] {
+            return api.rope_append(&c->cfg, q.p, q.s0, q.s1, qo.p, qo.s0, qo.s1, kn.p, kn.s0, kn.s1, vn.p, vn.s0, vn.s1, k.p,
+                                   k.s0, k.s1, k.s2, v.p, v.s0, v.s1, v.s2, (int32_t)tokens, (int32_t)hq, (int32_t)heads,
+                                   (int32_t)dv, (int32_t)page, (int32_t)pages, c->turns, (const int64_t*)pos.p,
+                                   (const int64_t*)slots.p, stream);
+        });
+}
+
+int rope_init(PyObject* self, PyObject* args, PyObject*) {
+    Rope* c = (Rope*)self;
+    Py_buffer cfg;
+    unsigned long long turns;
+    if (!PyArg_ParseTuple(args, "y*Ki", &cfg, &turns, &c->device)) return -1;
+    const bool ok = cfg.len == (Py_ssize_t)sizeof c->cfg;
+    if (ok) memcpy(&c->cfg, cfg.buf, sizeof c->cfg);
+    PyBuffer_Release(&cfg);
+    if (!ok) PyErr_SetString(PyExc_ValueError, "configuration of another size");
+    c->turns = (const uint64_t*)(uintptr_t)turns;
+    return ok ? 0 : -1;
+}
+
+PyMethodDef rope_methods[] = {
+    {"rotate", (PyCFunction)(void (*)(void))rope_rotate, METH_FASTCALL, "rotate(x, positions, out, inverse) -> status or -1"},
+    {"append", (PyCFunction)(void (*)(void))rope_append, METH_FASTCALL,
+     "append(q, k_new, v_new, k_pages, v_pages, slot_mapping, positions, q_out) -> status or -1"},
+    {nullptr, nullptr, 0, nullptr}};
+
+PyTypeObject RopeType = {PyVarObject_HEAD_INIT(nullptr, 0)};
+
+// ---------------------------------------------------------------------------------------------
+// attention to selected blocks
+// ---------------------------------------------------------------------------------------------
+struct Block {
+    PyObject_HEAD
+    vpp_block_attn_config_t cfg;
+    int device;
+    const vpp_query_block_t* entries;  // of the plan, on the device
+    int64_t num_entries, tokens, segments, seg_rows, max_kv_len, ws_bytes;
+    void* plan_stream;  // the stream that the entries were copied on
+};
+
+// Plain summaries, queries, table and lists of the planned chunk, for a launch on the stream of
+// the plan (on another the wrapper orders the two).
+bool planned(const Block* c, const at::Tensor* q, const at::Tensor* bt, const at::Tensor* lists, int64_t page, void*& stream) {
+    if (!c->entries || !q || !bt || !lists || (int)c10::hip::current_device() != c->device) return false;
+    if (q->size(0) < c->tokens || q->size(1) != c->cfg.num_q_heads || q->size(2) != c->cfg.head_dim_qk) return false;
+    if (lists->size(0) != c->num_entries || lists->size(1) != c->cfg.num_kv_heads || lists->size(2) != c->cfg.max_blocks ||
+        !lists->is_contiguous())
+        return false;
+    if (bt->size(0) < c->segments || c->seg_rows > bt->size(1) * page || !fits32({page, bt->size(1)})) return false;
+    stream = stream_of(c->device);
+    return stream == c->plan_stream;
+}
+
+// summarize(k_pages, blocks, summaries)
+PyObject* block_summarize(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+    const Block* c = (Block*)self;
+    View k, ids, sums;
+    int64_t pages = 0, page = 0, count = 0;
+    void* stream = nullptr;
+    return checked_call(
+        [&] {
+            if (n != 3 || (int)c10::hip::current_device() != c->device) return false;
+            const at::Tensor *tk = plain(a[0], c->device, at::kBFloat16, 4), *ts = plain(a[2], c->device, at::kBFloat16, 4);
+            const at::Tensor* ti = plain(a[1], c->device, at::kLong, 1);
+            if (!tk || !ts || !ti || !ts->is_contiguous()) return false;
+            pages = tk->size(0), page = tk->size(1), count = ti->size(0);
+            if (tk->size(2) != c->cfg.num_kv_heads || tk->size(3) != c->cfg.head_dim_qk || !fits32({pages, page, count})) return false;
+            if (ts->size(0) != pages || ts->size(1) * c->cfg.block_size != page || ts->size(2) != tk->size(2) ||
+                ts->size(3) != tk->size(3))
+                return false;
+            k = View(tk), ids = View(ti), sums = View(ts);
+            stream = stream_of(c->device);
+            return true;
+        },
+        [&] {
+            return api.block_summarize(&c->cfg, k.p, k.s0, k.s1, k.s2, (int32_t)page, (int32_t)pages, (const int64_t*)ids.p,
+                                       (int32_t)count, sums.p, stream);
+        });
+}
+
+// select(q, summaries, block_table, blocks)
+PyObject* block_select(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+    const Block* c = (Block*)self;
+    View q, sums, bt, lists;
+    int64_t pages = 0, page = 0, per_row = 0;
+    void* stream = nullptr;
+    return checked_call(
+        [&] {
+            if (n != 4) return false;
+            const at::Tensor *tq = plain(a[0], c->device, at::kBFloat16, 3), *ts = plain(a[1], c->device, at::kBFloat16, 4);
+            const at::Tensor *tb = plain(a[2], c->device, at::kInt, 2), *tl = plain(a[3], c->device, at::kInt, 3);
+            if (!ts || !ts->is_contiguous() || ts->size(2) != c->cfg.num_kv_heads || ts->size(3) != c->cfg.head_dim_qk) return false;
+            pages = ts->size(0), page = ts->size(1) * c->cfg.block_size;
+            if (!fits32({pages}) || !planned(c, tq, tb, tl, page, stream)) return false;
+            per_row = tb->size(1);
+            q = View(tq), sums = View(ts), bt = View(tb), lists = View(tl);
+            return true;
+        },
+        [&] {
+            return api.block_select(&c->cfg, c->entries, (int32_t)c->num_entries, q.p, q.s0, q.s1, (int32_t)c->tokens, sums.p,
+                                    (int32_t)page, (int32_t)pages, (const int32_t*)bt.p, bt.s0, (int32_t)c->segments,
+                                    (int32_t)per_row, c->max_kv_len, (int32_t*)lists.p, stream);
+        });
+}
+
+// run_paged(q, k_pages, v_pages, block_table, blocks, out, lse or None)
+PyObject* block_run(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+    const Block* c = (Block*)self;
+    View q, k, v, bt, lists, out, lse, ws;
+    at::Tensor scratch;  // of the stream's own memory, so that it is free again in the stream's order
+    int64_t pages = 0, page = 0, per_row = 0;
+    void* stream = nullptr;
+    return checked_call(
+        [&] {
+            if (n != 7) return false;
+            const at::Tensor *tq = plain(a[0], c->device, at::kBFloat16, 3), *to = plain(a[5], c->device, at::kBFloat16, 3);
+            const at::Tensor *tk = plain(a[1], c->device, at::kBFloat16, 4), *tv = plain(a[2], c->device, at::kBFloat16, 4);
+            const at::Tensor *tb = plain(a[3], c->device, at::kInt, 2), *tl = plain(a[4], c->device, at::kInt, 3);
+            if (!tk || !tv || !to) return false;
+            pages = tk->size(0), page = tk->size(1);
+            if (tk->size(2) != c->cfg.num_kv_heads || tk->size(3) != c->cfg.head_dim_qk || tv->size(0) != pages ||
+                tv->size(1) != page || tv->size(2) != tk->size(2) || tv->size(3) != c->cfg.head_dim_v)
+                return false;
+            if (!fits32({pages}) || !planned(c, tq, tb, tl, page, stream)) return false;
+            if (to->size(0) < c->tokens || to->size(1) != c->cfg.num_q_heads || to->size(2) != c->cfg.head_dim_v) return false;
+            if (a[6] != Py_None) {
+                const at::Tensor* t = plain(a[6], c->device, at::kFloat, 2);
+                if (!t || t->size(0) != c->cfg.num_q_heads || t->size(1) < c->tokens) return false;
+                lse = View(t);
+            }
+            if (c->ws_bytes > 0) {
+                scratch = at::empty({c->ws_bytes}, tq->options().dtype(at::kByte));
+                ws = View(&scratch);
+            }
+            per_row = tb->size(1);
+            q = View(tq), k = View(tk), v = View(tv), bt = View(tb), lists = View(tl), out = View(to);
+            return true;
+        },
+        [&] {
+            return api.block_run(&c->cfg, c->entries, (int32_t)c->num_entries, q.p, q.s0, q.s1, (int32_t)c->tokens, k.p, k.s0,
+                                 k.s1, k.s2, v.p, v.s0, v.s1, v.s2, (int32_t)page, (int32_t)pages, (const int32_t*)bt.p, bt.s0,
+                                 (int32_t)c->segments, (int32_t)per_row, (const int32_t*)lists.p, out.p, out.s0, out.s1,
+                                 (float*)lse.p, lse.s0, ws.p, (size_t)c->ws_bytes, stream);
+        });
+}
+
+PyObject* block_set_plan(PyObject* self, PyObject* args) {
+    Block* c = (Block*)self;
+    unsigned long long entries, stream;
+    long long x[6];
+    if (!PyArg_ParseTuple(args, "KLLLLLLK", &entries, &x[0], &x[1], &x[2], &x[3], &x[4], &x[5], &stream)) return nullptr;
+    c->entries = (const vpp_query_block_t*)(uintptr_t)entries;
+    c->num_entries = x[0];
+    c->tokens = x[1];
+    c->segments = x[2];
+    c->seg_rows = x[3];
+    c->max_kv_len = x[4];
+    c->ws_bytes = x[5];
+    c->plan_stream = (void*)(uintptr_t)stream;
+    Py_RETURN_NONE;
+}
+
+int block_init(PyObject* self, PyObject* args, PyObject*) {
+    Block* c = (Block*)self;
+    Py_buffer cfg;
+    if (!PyArg_ParseTuple(args, "y*i", &cfg, &c->device)) return -1;
+    const bool ok = cfg.len == (Py_ssize_t)sizeof c->cfg;
+    if (ok) memcpy(&c->cfg, cfg.buf, sizeof c->cfg);
+    PyBuffer_Release(&cfg);
+    if (!ok) PyErr_SetString(PyExc_ValueError, "configuration of another size");
+    c->entries = nullptr;
+    return ok ? 0 : -1;
+}
+
+PyMethodDef block_methods[] = {
+    {"set_plan", block_set_plan, METH_VARARGS,
+     "set_plan(query blocks, their number, tokens, segments, seg_rows, max_kv_len, workspace bytes, stream)"},
+    {"summarize", (PyCFunction)(void (*)(void))block_summarize, METH_FASTCALL, "summarize(k_pages, blocks, summaries) -> status or -1"},
+    {"select", (PyCFunction)(void (*)(void))block_select, METH_FASTCALL, "select(q, summaries, block_table, blocks)"},
+    {"run_paged", (PyCFunction)(void (*)(void))block_run, METH_FASTCALL,
+     "run_paged(q, k_pages, v_pages, block_table, blocks, out, lse)"},
+    {nullptr, nullptr, 0, nullptr}};
+
+PyTypeObject BlockType = {PyVarObject_HEAD_INIT(nullptr, 0)};
+
 PyMethodDef caller_methods[] = {
     {"set_plan", call_set_plan, METH_VARARGS, "set_plan(handle or 0, tokens, max_row, segments, seg_rows)"},
     {"run", (PyCFunction)(void (*)(void))call_run, METH_FASTCALL, "run(q, k, v, out, lse, workspace) -> status or -1"},
@@ -287,7 +559,19 @@ PyObject* bind(PyObject*, PyObject* args) {
     Py_RETURN_NONE;
 }
 
+PyObject* bind_sparse(PyObject*, PyObject* args) {
+    unsigned long long p[5];
+    if (!PyArg_ParseTuple(args, "KKKKK", &p[0], &p[1], &p[2], &p[3], &p[4])) return nullptr;
+    api.rope = (decltype(api.rope))(uintptr_t)p[0];
+    api.rope_append = (decltype(api.rope_append))(uintptr_t)p[1];
+    api.block_summarize = (decltype(api.block_summarize))(uintptr_t)p[2];
+    api.block_select = (decltype(api.block_select))(uintptr_t)p[3];
+    api.block_run = (decltype(api.block_run))(uintptr_t)p[4];
+    Py_RETURN_NONE;
+}
+
 PyMethodDef module_methods[] = {
+    {"bind_sparse", bind_sparse, METH_VARARGS, "bind_sparse(rope, rope_append, block_summarize, block_select, block_run)"},
     {"bind", bind, METH_VARARGS, "bind(run, run_noalloc, run_mla, run_paged, append): addresses of the C entry points"},
     {"append", (PyCFunction)(void (*)(void))call_append, METH_FASTCALL,
      "append(k_new, v_new, k_pages, v_pages, slot_mapping) -> status or -1"},
@@ -311,5 +595,24 @@ PyMODINIT_FUNC PyInit_vpp_torch(void) {
     if (!m) return nullptr;
     Py_INCREF(&CallerType);
     if (PyModule_AddObject(m, "Caller", (PyObject*)&CallerType) < 0) return nullptr;
+    struct {
+        PyTypeObject* type;
+        const char *name, *full;
+        Py_ssize_t size;
+        PyMethodDef* methods;
+        initproc init;
+    } const types[] = {{&RopeType, "Rope", "vpp_torch.Rope", sizeof(Rope), rope_methods, rope_init},
+                       {&BlockType, "Block", "vpp_torch.Block", sizeof(Block), block_methods, block_init}};
+    for (const auto& t : types) {
+        t.type->tp_name = t.full;
+        t.type->tp_basicsize = t.size;
+        t.type->tp_flags = Py_TPFLAGS_DEFAULT;
+        t.type->tp_methods = t.methods;
+        t.type->tp_init = t.init;
+        t.type->tp_new = PyType_GenericNew;
+        if (PyType_Ready(t.type) < 0) return nullptr;
+        Py_INCREF(t.type);
+        if (PyModule_AddObject(m, t.name, (PyObject*)t.type) < 0) return nullptr;
+    }
     return m;
 }

@@ -88,6 +88,14 @@ vpp_status_t vpp_block_summarize_paged(const vpp_block_attn_config_t* cfg,
                                        const int64_t* blocks, int32_t num_blocks, void* summaries, void* stream);
 
 /*
+ * Bytes of device workspace that vpp_block_select_paged needs (0: none): the scores of a slab of
+ * the query blocks, at most 256 MiB or those of 64 of them. Errors: VPP_ERR_INVALID_ARG,
+ * VPP_ERR_UNSUPPORTED (head dims; more than 32768 blocks up to max_kv_len).
+ */
+vpp_status_t vpp_block_select_workspace(const vpp_block_attn_config_t* cfg, int32_t num_query_blocks,
+                                        int64_t max_kv_len, size_t* bytes);
+
+/*
  * The lists: blocks[i][kv head][0 .. max_blocks - 1] (int32, contiguous) of query block i.
  * Of blocks 0 .. c, c that of the query block's last token, with f that of its first:
  *   - always on the list: b < sink_blocks, and b > f - local_blocks;
@@ -100,16 +108,18 @@ vpp_status_t vpp_block_summarize_paged(const vpp_block_attn_config_t* cfg,
  * query_blocks: device array; q as for the attention; summaries as above (those of blocks
  * without a written summary are read as they are; only complete blocks before f are
  * read). max_kv_len: an upper bound on kv positions of the chunk (its longest prefix + len);
- * blocks past it are not seen. block_table [num_segments][pages_per_row].
+ * blocks past it are not seen. block_table [num_segments][pages_per_row]. workspace:
+ * 256-byte aligned, may be NULL if the size is 0; not to be used by other work in flight.
  * Errors: VPP_ERR_INVALID_ARG; VPP_ERR_UNSUPPORTED (head dims; more than 32768 blocks up
- * to max_kv_len); VPP_ERR_HIP.
+ * to max_kv_len); VPP_ERR_WORKSPACE; VPP_ERR_HIP.
  */
 vpp_status_t vpp_block_select_paged(const vpp_block_attn_config_t* cfg,
                                     const vpp_query_block_t* query_blocks, int32_t num_query_blocks,
                                     const void* q, int64_t q_stride_tok, int64_t q_stride_head, int32_t num_tokens,
                                     const void* summaries, int32_t page_size, int32_t num_pages,
                                     const int32_t* block_table, int64_t block_table_stride, int32_t num_segments,
-                                    int32_t pages_per_row, int64_t max_kv_len, int32_t* blocks, void* stream);
+                                    int32_t pages_per_row, int64_t max_kv_len, int32_t* blocks,
+                                    void* workspace, size_t workspace_bytes, void* stream);
 
 /*
  * Bytes of device workspace that vpp_block_attn_run_paged needs for a chunk of num_tokens

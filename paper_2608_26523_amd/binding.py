@@ -33,8 +33,8 @@ EXPORTED = [
 # the entry points of vpp_rope.h and of vpp_block_attn.h
 EXPORTED_ROPE = ["vpp_rope_turns", "vpp_rope", "vpp_rope_append_paged"]
 EXPORTED_BLOCK = [
-    "vpp_query_blocks", "vpp_completed_blocks", "vpp_block_summarize_paged", "vpp_block_select_paged",
-    "vpp_block_attn_workspace", "vpp_block_attn_run_paged",
+    "vpp_query_blocks", "vpp_completed_blocks", "vpp_block_summarize_paged", "vpp_block_select_workspace",
+    "vpp_block_select_paged", "vpp_block_attn_workspace", "vpp_block_attn_run_paged",
 ]
 
 # bytes of the static device scratch behind vpp_chunk_attn_run_noalloc
@@ -150,6 +150,15 @@ def load(path: Optional[str] = None):
                                         i32, i32, i32, i32, i32, i32, vp, vp]
     lib.vpp_paged_slot_mapping.restype = ctypes.c_int
     lib.vpp_paged_slot_mapping.argtypes = [i32, vp, vp, vp, vp, i64, i32, i32, vp]
+    if hasattr(lib, "vpp_rope"):  # not in a build of the chunk attention alone
+        _declare_sparse(lib)
+    if path == LIB_PATH:
+        _lib = lib
+    return lib
+
+
+def _declare_sparse(lib):
+    vp, i32, i64, sz = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t
     lib.vpp_rope_turns.argtypes = [i32, vp, vp]
     lib.vpp_rope.argtypes = [ctypes.POINTER(RopeConfig), vp, i64, i64, vp, i64, i64, i32, i32, vp, vp, i32, vp]
     lib.vpp_rope_append_paged.argtypes = [ctypes.POINTER(RopeConfig), vp, i64, i64, vp, i64, i64, vp, i64, i64,
@@ -160,15 +169,13 @@ def load(path: Optional[str] = None):
     lib.vpp_query_blocks.argtypes = [i32, vp, vp, vp, i32, i32, vp, i32, count]
     lib.vpp_completed_blocks.argtypes = [i32, vp, vp, vp, vp, i64, i32, i32, i32, vp, i32, count]
     lib.vpp_block_summarize_paged.argtypes = [blk, vp, i64, i64, i64, i32, i32, vp, i32, vp, vp]
-    lib.vpp_block_select_paged.argtypes = [blk, vp, i32, vp, i64, i64, i32, vp, i32, i32, vp, i64, i32, i32, i64, vp, vp]
+    lib.vpp_block_select_paged.argtypes = [blk, vp, i32, vp, i64, i64, i32, vp, i32, i32, vp, i64, i32, i32, i64, vp, vp, sz, vp]
+    lib.vpp_block_select_workspace.argtypes = [blk, i32, i64, ctypes.POINTER(sz)]
     lib.vpp_block_attn_workspace.argtypes = [blk, i32, i32, ctypes.POINTER(sz)]
     lib.vpp_block_attn_run_paged.argtypes = [blk, vp, i32, vp, i64, i64, i32, vp, i64, i64, i64, vp, i64, i64, i64,
                                              i32, i32, vp, i64, i32, i32, vp, vp, i64, i64, vp, i64, vp, sz, vp]
     for name in EXPORTED_ROPE + EXPORTED_BLOCK:
         getattr(lib, name).restype = ctypes.c_int
-    if path == LIB_PATH:
-        _lib = lib
-    return lib
 
 
 _torch_ext = None
@@ -377,10 +384,16 @@ def vpp_block_summarize_paged(cfg: BlockConfig, k_ptr: int, k_sp: int, k_st: int
 def vpp_block_select_paged(cfg: BlockConfig, qb_ptr: int, num_query_blocks: int, q_ptr: int, q_st: int, q_sh: int,
                            num_tokens: int, summaries_ptr: int, page_size: int, num_pages: int, bt_ptr: int,
                            bt_st: int, num_segments: int, pages_per_row: int, max_kv_len: int, blocks_ptr: int,
-                           stream: int) -> None:
+                           ws_ptr: int, ws_bytes: int, stream: int) -> None:
     _call("vpp_block_select_paged", ctypes.byref(cfg), qb_ptr, num_query_blocks, q_ptr, q_st, q_sh, num_tokens,
           summaries_ptr, page_size, num_pages, bt_ptr, bt_st, num_segments, pages_per_row, max_kv_len, blocks_ptr,
-          stream)
+          ws_ptr, ws_bytes, stream)
+
+
+def vpp_block_select_workspace(cfg: BlockConfig, num_query_blocks: int, max_kv_len: int) -> int:
+    n = ctypes.c_size_t(0)
+    _call("vpp_block_select_workspace", ctypes.byref(cfg), num_query_blocks, max_kv_len, ctypes.byref(n))
+    return n.value
 
 
 def vpp_block_attn_workspace(cfg: BlockConfig, num_query_blocks: int, num_tokens: int) -> int:

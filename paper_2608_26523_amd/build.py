@@ -11,7 +11,7 @@ import sys
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 SRC = os.path.join(PKG, "csrc", "vpp_chunk_attn.hip")
-MORE_SRCS = [os.path.join(PKG, "csrc", name) for name in ("vpp_rope.hip", "vpp_block_attn.hip")]
+MORE_SRCS = [os.path.join(PKG, "csrc", name) for name in ("vpp_rope.hip", "vpp_block_select.hip", "vpp_block_attn.hip")]
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "libvpp_chunk_attn.so")
 SCHED_SRC = os.path.join(PKG, "csrc", "vpp_sched.cpp")

@@ -1,317 +1,7 @@
-// vpp_block_attn.hip -- attention to selected blocks of a paged KV cache for MI355X (gfx950):
-// block summaries, block selection, and the attention itself.
-#include <hip/hip_runtime.h>
-
-#include <math.h>
-#include <stdint.h>
-
-#include <type_traits>
-#include <utility>
-
-#include "vpp_block_attn.h"
+// vpp_block_attn.hip -- attention to selected blocks of a paged KV cache for MI355X (gfx950).
+#include "vpp_block_common.h"
 
 namespace {
-
-typedef uint16_t u16;
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
-typedef short i16x4 __attribute__((ext_vector_type(4)));
-typedef __attribute__((address_space(3))) void lds_void_t;
-
-constexpr int NWAVES = 4;
-constexpr int NTHREADS = 64 * NWAVES;
-constexpr int BN = 64;               // keys of a tile
-constexpr int MAX_LIST = 2048;       // entries of a list
-constexpr int MAX_CANDIDATES = 32768;  // blocks that a selection looks at
-constexpr float LOG2E = 1.4426950408889634f;
-constexpr float LN2 = 0.6931471805599453f;
-
-// Values of a vector count at most 2^60, and its grid's step is at least 2^-62: the product of
-// two steps is a normal number and a sum of 192 products below 2^128.
-constexpr float GRID_MOST = 0x1p60f;
-constexpr int GRID_MIN_EXP = -54;
-
-__device__ __forceinline__ int count(uint64_t mask) { return (int)__popcll(mask); }
-__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
-
-// The value and its neighbour's 16 or 32 lanes further, combined.
-__device__ __forceinline__ float max_xor16(float x) {
-    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
-}
-__device__ __forceinline__ float max_xor32(float x) {
-    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
-}
-__device__ __forceinline__ float sum_groups(float x) {  // over the four 16-lane groups
-    auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-    x = __uint_as_float(r[0]) + __uint_as_float(r[1]);
-    r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
-}
-
-// The page of a cache row, whatever the table holds.
-struct Pages {
-    const int32_t* table;
-    int64_t table_st;
-    int32_t pages_per_row, num_pages, page_shift;
-    __device__ __forceinline__ int page(int segment, int row) const {
-        const int i = min(row >> page_shift, pages_per_row - 1);
-        return (int)min((uint32_t)table[(int64_t)segment * table_st + i], (uint32_t)(num_pages - 1));
-    }
-};
-
-// A query block as the device reads it; rows = 0 if it is none of this chunk's.
-struct Entry {
-    int row0, rows, segment, pos0, kv_start;
-};
-__device__ __forceinline__ Entry load_entry(const vpp_query_block_t* blocks, int i, int query_block, int tokens, int segments) {
-    const vpp_query_block_t b = blocks[i];
-    Entry e{uniform(b.row0), uniform(b.rows), uniform(b.segment), uniform(b.pos0), uniform(b.kv_start)};
-    e.rows = min(e.rows, query_block);
-    const bool bad = e.rows < 0 || e.row0 < 0 || e.row0 > tokens - e.rows || e.segment < 0 || e.segment >= segments ||
-                     e.pos0 < 0 || e.kv_start < 0 || e.pos0 > INT32_MAX - e.kv_start - 256;
-    if (bad) e = Entry{0, 0, 0, 0, 0};
-    e.kv_start &= ~(BN - 1);  // so that no tile of keys leaves its page
-    return e;
-}
-
-// ---------------------------------------------------------------------------------------------
-// summaries
-// ---------------------------------------------------------------------------------------------
-struct SummarizeArgs {
-    const u16* k;
-    u16* summaries;
-    const int64_t* blocks;
-    int64_t k_sp, k_st, k_sh;
-    int64_t total;  // blocks of the cache
-    int32_t hkv, block, per_page_shift;
-};
-
-// One workgroup a (block, kv head). Bound by HBM: the keys are read once, 16 bytes a load; a
-// thread sums 8 dims of every RS-th row in 64 bits, which is exact for keys within 2^37 of the
-// largest, so the order of the sum does not show.
-template <int DQK>
-__global__ __launch_bounds__(NTHREADS) void summarize_kernel(SummarizeArgs a) {
-    constexpr int GR = DQK / 8, RS = NTHREADS / GR;  // granules of a row, rows at a time
-    __shared__ double part[RS][DQK];
-    __shared__ float top[NWAVES];
-    const int head = (int)blockIdx.x % a.hkv, n = (int)blockIdx.x / a.hkv;
-    const int64_t block = a.blocks[n];
-    if (block < 0 || block >= a.total) return;
-    const int64_t page = block >> a.per_page_shift;
-    const int row0 = (int)(block & ((1 << a.per_page_shift) - 1)) * a.block;
-    const u16* const base = a.k + page * a.k_sp + (int64_t)row0 * a.k_st + (int64_t)head * a.k_sh;
-    const int g = (int)threadIdx.x % GR, r0 = (int)threadIdx.x / GR;
-    if (r0 < RS) {
-        double sum[8] = {};
-        for (int r = r0; r < a.block; r += RS) {
-            const bf16x8 x = *(const bf16x8*)(base + (int64_t)r * a.k_st + g * 8);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) sum[i] += (double)(float)x[i];
-        }
-#pragma unroll
-        for (int i = 0; i < 8; ++i) part[r0][g * 8 + i] = sum[i];
-    }
-    __syncthreads();
-    const int d = (int)threadIdx.x;
-    double mean = 0;
-    if (d < DQK) {
-#pragma unroll
-        for (int r = 0; r < RS; ++r) mean += part[r][d];
-        mean /= a.block;
-        mean = mean == mean ? fmin(fmax(mean, -(double)GRID_MOST), (double)GRID_MOST) : 0;
-    }
-    // the exponent of the largest: of the mean as it is, or (rounded up to fp32) no smaller
-    float m = __double2float_rz(fabs(mean));  // the same power of two below
-#pragma unroll
-    for (int s = 1; s < 64; s *= 2) m = fmaxf(m, __shfl_xor(m, s));
-    if (d % 64 == 0) top[d / 64] = m;
-    __syncthreads();
-    m = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
-    const int e = max(m > 0 ? ilogbf(m) + 1 : GRID_MIN_EXP, GRID_MIN_EXP);
-    if (d < DQK) {
-        const double v = ldexp(rint(ldexp(mean, 8 - e)), e - 8);
-        const __bf16 r = (__bf16)(float)v;  // exact: 8 bits
-        a.summaries[(block * a.hkv + head) * DQK + d] = __builtin_bit_cast(u16, r);
-    }
-}
-
-// ---------------------------------------------------------------------------------------------
-// selection
-// ---------------------------------------------------------------------------------------------
-struct SelectArgs {
-    const u16* q;
-    const u16* summaries;
-    const vpp_query_block_t* entries;
-    int32_t* lists;
-    int64_t q_st, q_sh;
-    Pages pages;
-    int32_t num_entries, tokens, segments, query_block, group, hkv;
-    int32_t block_shift, sink, local, max_blocks, cap;  // cap: blocks that the scores have room for
-    int32_t wg_entries, rows;                           // query blocks of a workgroup; MFMA rows of one
-};
-
-// A score as an unsigned number of the same order, at least 1.
-__device__ __forceinline__ uint32_t order_key(float x) {
-    const uint32_t u = __float_as_uint(x + 0.f);  // -0 becomes 0
-    return u & 0x80000000u ? ~u : u | 0x80000000u;
-}
-
-// Scores are products of MFMA tiles of 16 query rows x 16 blocks, in LDS as keys of their order;
-// then a wave a query block finds the smallest selected key bit by bit and writes the list.
-template <int DQK>
-__global__ __launch_bounds__(NTHREADS) void select_kernel(SelectArgs a) {
-    constexpr int KS = DQK / 32, MT = 4;  // MFMA steps of a product, row tiles at a time
-    extern __shared__ uint32_t keys[];    // [wg_entries][cap]
-    const int lane = (int)threadIdx.x & 63, wave = uniform((int)threadIdx.x >> 6);
-    const int head = (int)blockIdx.x % a.hkv, entry0 = (int)blockIdx.x / a.hkv * a.wg_entries;
-    const int entries = min(a.wg_entries, a.num_entries - entry0);
-    const int col = lane & 15, grp = lane >> 4;
-    for (int i = threadIdx.x; i < entries * a.cap; i += NTHREADS) keys[i] = 0;
-    __syncthreads();
-
-    auto entry = [&](int i) { return load_entry(a.entries, entry0 + i, a.query_block, a.tokens, a.segments); };
-    // blocks [lo, hi) of a query block compete for its list; last: that of its last token
-    auto range = [&](const Entry& e, int& lo, int& hi, int& last) {
-        last = min((e.pos0 + e.rows - 1) >> a.block_shift, a.cap - 1);
-        lo = a.sink;
-        hi = min((e.pos0 >> a.block_shift) - a.local + 1, last + 1);
-        if (hi < lo || last + 1 <= a.max_blocks) hi = lo;  // nothing to choose
-    };
-    const int tiles = (entries * a.rows + 15) / 16;
-    for (int done = 0; done < entries;) {
-        // the next query blocks, of one segment
-        const int segment = entry(done).segment;
-        int next = done, lo = a.cap, hi = 0, kv_start = 0;
-        for (; next < entries; ++next) {
-            const Entry e = entry(next);
-            if (e.rows == 0) continue;
-            if (e.segment != segment) break;
-            int l, h, last;
-            range(e, l, h, last);
-            if (h > l) lo = min(lo, l), hi = max(hi, h);
-            kv_start = e.kv_start;
-        }
-        const int first = done;
-        done = next == done ? done + 1 : next;
-        if (hi <= lo) continue;
-        for (int mt0 = first * a.rows / 16; mt0 < min((done * a.rows + 15) / 16, tiles); mt0 += MT) {
-            // query rows on their grid, as A operands
-            bf16x8 qf[MT][KS];
-#pragma unroll
-            for (int m = 0; m < MT; ++m) {
-                const int slot = (mt0 + m) * 16 + col;
-                const int ei = min(slot / a.rows, entries - 1);
-                const vpp_query_block_t b = a.entries[entry0 + ei];
-                const int rows = min(max(min(b.rows, a.query_block), 0), a.tokens);
-                const int r = min(slot % a.rows, max(rows * a.group - 1, 0));  // rows past the last repeat it
-                const int token = min(min(max(b.row0, 0), a.tokens - 1) + r / a.group, a.tokens - 1);
-                const u16* const p = a.q + (int64_t)token * a.q_st + (int64_t)(head * a.group + r % a.group) * a.q_sh + grp * 8;
-                float x[KS][8], top = 0;
-#pragma unroll
-                for (int s = 0; s < KS; ++s) {
-                    const bf16x8 y = *(const bf16x8*)(p + s * 32);
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const float v = (float)y[i];
-                        x[s][i] = v == v ? fminf(fmaxf(v, -GRID_MOST), GRID_MOST) : 0.f;
-                        top = fmaxf(top, fabsf(x[s][i]));
-                    }
-                }
-                top = max_xor32(max_xor16(top));
-                const int e = max(top > 0 ? ilogbf(top) + 1 : GRID_MIN_EXP, GRID_MIN_EXP);
-                const float up = ldexpf(1.f, 8 - e), down = ldexpf(1.f, e - 8);
-#pragma unroll
-                for (int s = 0; s < KS; ++s)
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) qf[m][s][i] = (__bf16)(rintf(x[s][i] * up) * down);
-            }
-            for (int t0 = lo + wave * 16; t0 < hi; t0 += NWAVES * 16) {
-                const int b = min(t0 + col, hi - 1);
-                const int row = kv_start + (b << a.block_shift);
-                const int page = a.pages.page(segment, row);
-                const int64_t at = ((int64_t)page << (a.pages.page_shift - a.block_shift)) +
-                                   ((row & ((1 << a.pages.page_shift) - 1)) >> a.block_shift);
-                const u16* const p = a.summaries + (at * a.hkv + head) * DQK + grp * 8;
-                bf16x8 kf[KS];
-#pragma unroll
-                for (int s = 0; s < KS; ++s) kf[s] = *(const bf16x8*)(p + s * 32);
-#pragma unroll
-                for (int m = 0; m < MT; ++m) {
-                    if (mt0 + m >= tiles) break;
-                    f32x4 d = {0, 0, 0, 0};
-#pragma unroll
-                    for (int s = 0; s < KS; ++s) d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(qf[m][s], kf[s], d, 0, 0, 0);
-                    // d[i]: row (mt0 + m) * 16 + grp * 4 + i, block t0 + col
-                    const int slot = (mt0 + m) * 16 + grp * 4;
-                    auto put = [&](int ei, float v, bool mine) {
-                        if (mine && ei >= first && ei < done && t0 + col < hi) {
-                            uint32_t& k = keys[ei * a.cap + t0 + col];
-                            k = max(k, order_key(v));
-                        }
-                    };
-                    if (a.rows == 1) {
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) put(slot + i, d[i], true);
-                    } else if (a.rows == 2) {
-                        put(slot / 2, fmaxf(d[0], d[1]), true);
-                        put(slot / 2 + 1, fmaxf(d[2], d[3]), true);
-                    } else {
-                        float v = fmaxf(fmaxf(d[0], d[1]), fmaxf(d[2], d[3]));
-                        if (a.rows >= 8) v = max_xor16(v);
-                        if (a.rows >= 16) v = max_xor32(v);
-                        put(slot / a.rows, v, a.rows == 4 || (a.rows == 8 && grp % 2 == 0) || grp == 0);
-                    }
-                }
-            }
-        }
-    }
-    __syncthreads();
-
-    for (int ei = wave; ei < entries; ei += NWAVES) {
-        const Entry e = entry(ei);
-        int32_t* const list = a.lists + ((int64_t)(entry0 + ei) * a.hkv + head) * a.max_blocks;
-        const uint32_t* const key = keys + ei * a.cap;
-        int at = 0;
-        if (e.rows > 0) {
-            int lo, hi, last;
-            range(e, lo, hi, last);
-            const int want = hi > lo ? a.max_blocks - (last + 1 - (hi - lo)) : 0;
-            // the want-th largest key, from its highest bit down
-            uint32_t least = 0;
-            int equal = 0;
-            if (hi - lo > want) {
-                for (int bit = 31; bit >= 0; --bit) {
-                    const uint32_t t = least | 1u << bit;
-                    int n = 0;
-                    for (int b = lo; b < hi; b += 64) n += count(__ballot(b + lane < hi && key[min(b + lane, hi - 1)] >= t));
-                    if (n >= want) least = t;
-                }
-                int more = 0;
-                for (int b = lo; b < hi; b += 64) more += count(__ballot(b + lane < hi && key[min(b + lane, hi - 1)] > least));
-                equal = want - more;  // of those equal to it, the first ones
-            }
-            for (int b0 = 0; b0 <= last; b0 += 64) {
-                const int b = b0 + lane;
-                const bool seen = b <= last, rival = seen && b >= lo && b < hi;
-                const uint32_t k = rival ? key[b] : 0;
-                const uint64_t same = __ballot(rival && k == least);
-                const uint64_t below = ((uint64_t)1 << lane) - 1;
-                const bool take = seen && (!rival || k > least || (k == least && count(same & below) < equal));
-                equal -= count(same);
-                const uint64_t all = __ballot(take);
-                const int to = at + count(all & below);
-                if (take && to < a.max_blocks) list[to] = b;
-                at += count(all);
-            }
-        }
-        for (int i = min(at, a.max_blocks) + lane; i < a.max_blocks; i += 64) list[i] = -1;
-    }
-}
 
 // ---------------------------------------------------------------------------------------------
 // attention
@@ -395,7 +85,7 @@ __global__ __launch_bounds__(NTHREADS) void attend_kernel(AttendArgs a) {
 
     const int head = (int)blockIdx.x % a.hkv, item = (int)blockIdx.x / a.hkv;
     const int chunk = item % a.chunks, ei = item / a.chunks;
-    const Entry e = load_entry(a.entries, ei, a.query_block, a.tokens, a.segments);
+    const Entry e = uniform(checked_entry(a.entries[ei], a.query_block, a.tokens, a.segments));
     const int row0 = chunk * ROWS, rows = min(e.rows * a.group - row0, ROWS);  // of the query block's rows
     if (rows <= 0) return;
     const int end = e.pos0 + e.rows;  // cached positions of the segment so far
@@ -643,174 +333,7 @@ __global__ __launch_bounds__(NTHREADS) void attend_kernel(AttendArgs a) {
     }
 }
 
-// ---------------------------------------------------------------------------------------------
-// host
-// ---------------------------------------------------------------------------------------------
-bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
-bool stride_ok(int64_t s) { return s > 0 && s % 8 == 0; }
-int log2_of(int x) {
-    int s = 0;
-    while ((1 << s) < x) ++s;
-    return s;
-}
-
-vpp_status_t check_config(const vpp_block_attn_config_t* c) {
-    if (!c) return VPP_ERR_INVALID_ARG;
-    if (c->num_q_heads < 1 || c->num_kv_heads < 1 || c->num_q_heads % c->num_kv_heads) return VPP_ERR_INVALID_ARG;
-    if (c->num_q_heads / c->num_kv_heads > 128) return VPP_ERR_INVALID_ARG;
-    if (!isfinite(c->softmax_scale) || c->softmax_scale < 0) return VPP_ERR_INVALID_ARG;
-    if (c->block_size != 64 && c->block_size != 128 && c->block_size != 256) return VPP_ERR_INVALID_ARG;
-    if (c->query_block < 1 || c->query_block > 128) return VPP_ERR_INVALID_ARG;
-    if (c->sink_blocks < 0 || c->local_blocks < 1 || c->max_blocks < 1 || c->max_blocks > MAX_LIST) return VPP_ERR_INVALID_ARG;
-    const int64_t sure = (int64_t)c->sink_blocks + c->local_blocks + (c->query_block - 1 + c->block_size - 1) / c->block_size;
-    if (c->max_blocks < sure) return VPP_ERR_INVALID_ARG;
-    const int d = c->head_dim_qk, v = c->head_dim_v;
-    if (!((d == 64 && v == 64) || (d == 128 && v == 128) || (d == 192 && v == 128))) return VPP_ERR_UNSUPPORTED;
-    return VPP_OK;
-}
-
-bool page_ok(int32_t page_size, int32_t num_pages, int32_t block_size) {
-    return page_size >= block_size && page_size <= (1 << 20) && (page_size & (page_size - 1)) == 0 && num_pages >= 1;
-}
-
-bool table_ok(const int32_t* table, int64_t st, int32_t segments, int32_t pages_per_row) {
-    return table && ((uintptr_t)table & 3u) == 0 && segments >= 1 && pages_per_row >= 1 && (segments == 1 || st >= 0);
-}
-
-// [rows][heads][dim] strides in elements; the stride of a size of 1 is not used
-bool strides_ok(int64_t st, int64_t rows, int64_t st_most, int64_t sh, int64_t heads, int64_t dim) {
-    return (rows == 1 || (stride_ok(st) && st >= dim && st < st_most)) &&
-           (heads == 1 || (stride_ok(sh) && sh >= dim && sh < ((int64_t)1 << 31)));
-}
-
 }  // namespace
-
-extern "C" vpp_status_t vpp_query_blocks(int32_t num_segments, const int32_t* cu_q, const int64_t* kv_start,
-                                         const int64_t* prefix_len, int32_t query_block, int32_t block_size,
-                                         vpp_query_block_t* blocks, int32_t capacity, int32_t* count) {
-    if (num_segments < 0 || !cu_q || !count || capacity < 0 || (capacity > 0 && !blocks)) return VPP_ERR_INVALID_ARG;
-    if (query_block < 1 || query_block > 128 || (block_size != 64 && block_size != 128 && block_size != 256))
-        return VPP_ERR_INVALID_ARG;
-    if (num_segments > 0 && (!kv_start || !prefix_len)) return VPP_ERR_INVALID_ARG;
-    if (cu_q[0] != 0) return VPP_ERR_INVALID_ARG;
-    int32_t n = 0;
-    for (int s = 0; s < num_segments; ++s) {
-        const int64_t len = (int64_t)cu_q[s + 1] - cu_q[s];
-        if (len < 0 || kv_start[s] < 0 || prefix_len[s] < 0 || kv_start[s] % block_size) return VPP_ERR_INVALID_ARG;
-        const int64_t most = INT32_MAX - 256;
-        if (kv_start[s] > most || prefix_len[s] > most || kv_start[s] + prefix_len[s] + len > most) return VPP_ERR_INVALID_ARG;
-        for (int64_t r = 0; r < len; r += query_block, ++n)
-            if (n < capacity)
-                blocks[n] = vpp_query_block_t{(int32_t)(cu_q[s] + r), (int32_t)(len - r < query_block ? len - r : query_block), s,
-                                              (int32_t)(prefix_len[s] + r), (int32_t)kv_start[s], {0, 0, 0}};
-    }
-    *count = n;
-    return VPP_OK;
-}
-
-extern "C" vpp_status_t vpp_completed_blocks(int32_t num_segments, const int32_t* cu_q, const int64_t* kv_start,
-                                             const int64_t* prefix_len, const int32_t* block_table,
-                                             int64_t block_table_stride, int32_t pages_per_row, int32_t page_size,
-                                             int32_t block_size, int64_t* blocks, int32_t capacity, int32_t* count) {
-    if (num_segments < 0 || !cu_q || !count || capacity < 0 || (capacity > 0 && !blocks)) return VPP_ERR_INVALID_ARG;
-    if ((block_size != 64 && block_size != 128 && block_size != 256) || !page_ok(page_size, 1, block_size))
-        return VPP_ERR_INVALID_ARG;
-    if (num_segments > 0 && (!kv_start || !prefix_len || !block_table)) return VPP_ERR_INVALID_ARG;
-    if (pages_per_row < 0 || block_table_stride < 0 || cu_q[0] != 0) return VPP_ERR_INVALID_ARG;
-    int32_t n = 0;
-    for (int s = 0; s < num_segments; ++s) {
-        const int64_t len = (int64_t)cu_q[s + 1] - cu_q[s];
-        if (len < 0 || kv_start[s] < 0 || prefix_len[s] < 0 || kv_start[s] % block_size) return VPP_ERR_INVALID_ARG;
-        const int64_t most = INT32_MAX - 256;
-        if (kv_start[s] > most || prefix_len[s] > most || kv_start[s] + prefix_len[s] + len > most) return VPP_ERR_INVALID_ARG;
-        const int64_t first = prefix_len[s] / block_size, last = (prefix_len[s] + len) / block_size;
-        for (int64_t b = first; b < last; ++b, ++n) {
-            const int64_t row = kv_start[s] + b * block_size, idx = row / page_size;
-            if (idx >= pages_per_row) return VPP_ERR_INVALID_ARG;
-            const int32_t page = block_table[(int64_t)s * block_table_stride + idx];
-            if (page < 0) return VPP_ERR_INVALID_ARG;
-            if (n < capacity) blocks[n] = (int64_t)page * (page_size / block_size) + row % page_size / block_size;
-        }
-    }
-    *count = n;
-    return VPP_OK;
-}
-
-extern "C" vpp_status_t vpp_block_summarize_paged(const vpp_block_attn_config_t* cfg, const void* k_pages, int64_t k_sp,
-                                                  int64_t k_st, int64_t k_sh, int32_t page_size, int32_t num_pages,
-                                                  const int64_t* blocks, int32_t num_blocks, void* summaries, void* stream) {
-    const vpp_status_t st = check_config(cfg);
-    if (st != VPP_OK) return st;
-    if (num_blocks < 0 || !page_ok(page_size, num_pages, cfg->block_size)) return VPP_ERR_INVALID_ARG;
-    if (num_blocks == 0) return VPP_OK;
-    if (!k_pages || !blocks || !summaries || !aligned16(k_pages) || !aligned16(summaries) || ((uintptr_t)blocks & 7u))
-        return VPP_ERR_INVALID_ARG;
-    const int hkv = cfg->num_kv_heads;
-    if (!strides_ok(k_st, page_size, (int64_t)1 << 31, k_sh, hkv, cfg->head_dim_qk) || (num_pages > 1 && !stride_ok(k_sp))) return VPP_ERR_INVALID_ARG;
-    if ((int64_t)num_blocks * hkv >= ((int64_t)1 << 31)) return VPP_ERR_INVALID_ARG;
-    SummarizeArgs a{};
-    a.k = (const u16*)k_pages;
-    a.summaries = (u16*)summaries;
-    a.blocks = blocks;
-    a.k_sp = k_sp; a.k_st = k_st; a.k_sh = k_sh;
-    a.per_page_shift = log2_of(page_size / cfg->block_size);
-    a.total = (int64_t)num_pages << a.per_page_shift;
-    a.hkv = hkv;
-    a.block = cfg->block_size;
-    auto* kernel = cfg->head_dim_qk == 64 ? summarize_kernel<64> : cfg->head_dim_qk == 128 ? summarize_kernel<128> : summarize_kernel<192>;
-    hipLaunchKernelGGL(kernel, dim3((unsigned)(num_blocks * hkv)), dim3(NTHREADS), 0, (hipStream_t)stream, a);
-    return hipGetLastError() == hipSuccess ? VPP_OK : VPP_ERR_HIP;
-}
-
-extern "C" vpp_status_t vpp_block_select_paged(const vpp_block_attn_config_t* cfg, const vpp_query_block_t* query_blocks,
-                                               int32_t num_query_blocks, const void* q, int64_t q_st, int64_t q_sh,
-                                               int32_t num_tokens, const void* summaries, int32_t page_size,
-                                               int32_t num_pages, const int32_t* block_table, int64_t bt_st,
-                                               int32_t num_segments, int32_t pages_per_row, int64_t max_kv_len,
-                                               int32_t* blocks, void* stream) {
-    const vpp_status_t st = check_config(cfg);
-    if (st != VPP_OK) return st;
-    if (num_query_blocks < 0 || num_tokens < 0 || max_kv_len < 0 || !page_ok(page_size, num_pages, cfg->block_size))
-        return VPP_ERR_INVALID_ARG;
-    if (num_query_blocks == 0 || num_tokens == 0) return VPP_OK;
-    if (!query_blocks || !q || !summaries || !blocks || !aligned16(query_blocks) || !aligned16(q) || !aligned16(summaries) ||
-        ((uintptr_t)blocks & 3u) || !table_ok(block_table, bt_st, num_segments, pages_per_row))
-        return VPP_ERR_INVALID_ARG;
-    if (!strides_ok(q_st, num_tokens, (int64_t)1 << 31, q_sh, cfg->num_q_heads, cfg->head_dim_qk)) return VPP_ERR_INVALID_ARG;
-    const int64_t cap = (max_kv_len + cfg->block_size - 1) / cfg->block_size;
-    if (cap > MAX_CANDIDATES) return VPP_ERR_UNSUPPORTED;
-    SelectArgs a{};
-    a.q = (const u16*)q;
-    a.summaries = (const u16*)summaries;
-    a.entries = query_blocks;
-    a.lists = blocks;
-    a.q_st = q_st;
-    a.q_sh = q_sh;
-    a.pages = Pages{block_table, bt_st, pages_per_row, num_pages, log2_of(page_size)};
-    a.num_entries = num_query_blocks;
-    a.tokens = num_tokens;
-    a.segments = num_segments;
-    a.query_block = cfg->query_block;
-    a.group = cfg->num_q_heads / cfg->num_kv_heads;
-    a.hkv = cfg->num_kv_heads;
-    a.block_shift = log2_of(cfg->block_size);
-    a.sink = cfg->sink_blocks;
-    a.local = cfg->local_blocks;
-    a.max_blocks = cfg->max_blocks;
-    a.cap = cap < 1 ? 1 : (int32_t)cap;
-    const int rows = a.group * a.query_block;
-    a.rows = rows <= 16 ? 1 << log2_of(rows) : (rows + 15) / 16 * 16;
-    a.wg_entries = 1;
-    const int64_t grid = (int64_t)((num_query_blocks + a.wg_entries - 1) / a.wg_entries) * a.hkv;
-    if (grid >= ((int64_t)1 << 31)) return VPP_ERR_INVALID_ARG;
-    const size_t lds = (size_t)a.wg_entries * a.cap * 4;
-    auto* kernel = cfg->head_dim_qk == 64 ? select_kernel<64> : cfg->head_dim_qk == 128 ? select_kernel<128> : select_kernel<192>;
-    if (lds > (64u << 10) &&
-        hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds) != hipSuccess)
-        return VPP_ERR_HIP;
-    hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(NTHREADS), lds, (hipStream_t)stream, a);
-    return hipGetLastError() == hipSuccess ? VPP_OK : VPP_ERR_HIP;
-}
 
 extern "C" vpp_status_t vpp_block_attn_workspace(const vpp_block_attn_config_t* cfg, int32_t num_query_blocks,
                                                  int32_t num_tokens, size_t* bytes) {

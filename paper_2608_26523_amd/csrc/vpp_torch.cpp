@@ -388,7 +388,7 @@ struct Block {
     vpp_block_attn_config_t cfg;
     int device;
     const vpp_query_block_t* entries;  // of the plan, on the device
-    int64_t num_entries, tokens, segments, seg_rows, max_kv_len, ws_bytes;
+    int64_t num_entries, tokens, segments, seg_rows, max_kv_len, ws_bytes, select_bytes;
     void* plan_stream;  // the stream that the entries were copied on
 };
 
@@ -435,7 +435,8 @@ PyObject* block_summarize(PyObject* self, PyObject* const* a, Py_ssize_t n) {
 // select(q, summaries, block_table, blocks)
 PyObject* block_select(PyObject* self, PyObject* const* a, Py_ssize_t n) {
     const Block* c = (Block*)self;
-    View q, sums, bt, lists;
+    View q, sums, bt, lists, ws;
+    at::Tensor scratch;  // of the stream's own memory, so that it is free again in the stream's order
     int64_t pages = 0, page = 0, per_row = 0;
     void* stream = nullptr;
     return checked_call(
@@ -445,7 +446,11 @@ PyObject* block_select(PyObject* self, PyObject* const* a, Py_ssize_t n) {
             const at::Tensor *tb = plain(a[2], c->device, at::kInt, 2), *tl = plain(a[3], c->device, at::kInt, 3);
             if (!ts || !ts->is_contiguous() || ts->size(2) != c->cfg.num_kv_heads || ts->size(3) != c->cfg.head_dim_qk) return false;
             pages = ts->size(0), page = ts->size(1) * c->cfg.block_size;
-            if (!fits32({pages}) || !planned(c, tq, tb, tl, page, stream)) return false;
+            if (c->select_bytes < 0 || !fits32({pages}) || !planned(c, tq, tb, tl, page, stream)) return false;
+            if (c->select_bytes > 0) {
+                scratch = at::empty({c->select_bytes}, tq->options().dtype(at::kByte));
+                ws = View(&scratch);
+            }
             per_row = tb->size(1);
             q = View(tq), sums = View(ts), bt = View(tb), lists = View(tl);
             return true;
@@ -453,7 +458,7 @@ PyObject* block_select(PyObject* self, PyObject* const* a, Py_ssize_t n) {
         [&] {
             return api.block_select(&c->cfg, c->entries, (int32_t)c->num_entries, q.p, q.s0, q.s1, (int32_t)c->tokens, sums.p,
                                     (int32_t)page, (int32_t)pages, (const int32_t*)bt.p, bt.s0, (int32_t)c->segments,
-                                    (int32_t)per_row, c->max_kv_len, (int32_t*)lists.p, stream);
+                                    (int32_t)per_row, c->max_kv_len, (int32_t*)lists.p, ws.p, (size_t)c->select_bytes, stream);
         });
 }
 
@@ -461,7 +466,7 @@ PyObject* block_select(PyObject* self, PyObject* const* a, Py_ssize_t n) {
 PyObject* block_run(PyObject* self, PyObject* const* a, Py_ssize_t n) {
     const Block* c = (Block*)self;
     View q, k, v, bt, lists, out, lse, ws;
-    at::Tensor scratch;  // of the stream's own memory, so that it is free again in the stream's order
+    at::Tensor scratch;
     int64_t pages = 0, page = 0, per_row = 0;
     void* stream = nullptr;
     return checked_call(
@@ -501,8 +506,8 @@ PyObject* block_run(PyObject* self, PyObject* const* a, Py_ssize_t n) {
 PyObject* block_set_plan(PyObject* self, PyObject* args) {
     Block* c = (Block*)self;
     unsigned long long entries, stream;
-    long long x[6];
-    if (!PyArg_ParseTuple(args, "KLLLLLLK", &entries, &x[0], &x[1], &x[2], &x[3], &x[4], &x[5], &stream)) return nullptr;
+    long long x[7];
+    if (!PyArg_ParseTuple(args, "KLLLLLLLK", &entries, &x[0], &x[1], &x[2], &x[3], &x[4], &x[5], &x[6], &stream)) return nullptr;
     c->entries = (const vpp_query_block_t*)(uintptr_t)entries;
     c->num_entries = x[0];
     c->tokens = x[1];
@@ -510,6 +515,7 @@ PyObject* block_set_plan(PyObject* self, PyObject* args) {
     c->seg_rows = x[3];
     c->max_kv_len = x[4];
     c->ws_bytes = x[5];
+    c->select_bytes = x[6];
     c->plan_stream = (void*)(uintptr_t)stream;
     Py_RETURN_NONE;
 }
@@ -528,7 +534,7 @@ int block_init(PyObject* self, PyObject* args, PyObject*) {
 
 PyMethodDef block_methods[] = {
     {"set_plan", block_set_plan, METH_VARARGS,
-     "set_plan(query blocks, their number, tokens, segments, seg_rows, max_kv_len, workspace bytes, stream)"},
+     "set_plan(query blocks, their number, tokens, segments, seg_rows, max_kv_len, workspace bytes of a run and of a selection, stream)"},
     {"summarize", (PyCFunction)(void (*)(void))block_summarize, METH_FASTCALL, "summarize(k_pages, blocks, summaries) -> status or -1"},
     {"select", (PyCFunction)(void (*)(void))block_select, METH_FASTCALL, "select(q, summaries, block_table, blocks)"},
     {"run_paged", (PyCFunction)(void (*)(void))block_run, METH_FASTCALL,

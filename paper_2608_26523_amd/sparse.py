@@ -54,7 +54,7 @@ class BlockSparseAttention:
         self.device = dev if dev.index is not None else torch.device("cuda", torch.cuda.current_device())
         self._native = ext.Block(bytes(self.cfg), self.device.index)
         self._qb: Optional[torch.Tensor] = None
-        self.tokens = self.num_query_blocks = self.workspace_bytes = 0
+        self.tokens = self.num_query_blocks = self.workspace_bytes = self.select_bytes = 0
 
     # -- planning -----------------------------------------------------------
     def plan(self, cu_q: Sequence[int], kv_start: Sequence[int], prefix_len: Sequence[int]) -> int:
@@ -70,6 +70,10 @@ class BlockSparseAttention:
         self.tokens = cu[-1]
         self.num_query_blocks = len(qb)
         self.workspace_bytes = B.vpp_block_attn_workspace(self.cfg, len(qb), self.tokens)
+        try:
+            self.select_bytes = B.vpp_block_select_workspace(self.cfg, len(qb), self.max_kv_len)
+        except B.VppError:  # more blocks than a selection takes: select() says so, lists of another kind run
+            self.select_bytes = -1
         with torch.cuda.device(self.device):
             host = torch.empty(max(1, 8 * len(qb)), dtype=torch.int32, pin_memory=True)
             host.numpy()[:8 * len(qb)] = qb.view("<i4").reshape(-1)
@@ -79,7 +83,7 @@ class BlockSparseAttention:
             self._copied = self._plan_stream.record_event()
         self._qb = dev
         self._native.set_plan(dev.data_ptr(), len(qb), self.tokens, self.segments, self.seg_rows, self.max_kv_len,
-                              self.workspace_bytes, self._plan_stream.cuda_stream)
+                              self.workspace_bytes, self.select_bytes, self._plan_stream.cuda_stream)
         return len(qb)
 
     def completed(self, cu_q: Sequence[int], kv_start: Sequence[int], prefix_len: Sequence[int], host_block_table,
@@ -188,11 +192,13 @@ class BlockSparseAttention:
         if blocks is None:
             blocks = new_on(s, (self.num_query_blocks, c.num_kv_heads, c.max_blocks), torch.int32)
         self._lists(blocks)
+        ws = new_on(s, (self.select_bytes,), torch.uint8) if self.select_bytes > 0 else None
         with torch.cuda.device(self.device):
             B.vpp_block_select_paged(c, self._qb.data_ptr(), self.num_query_blocks, q.data_ptr(), q.stride(0), q.stride(1),
                                      self.tokens, summaries.data_ptr(), page, int(summaries.shape[0]),
                                      block_table.data_ptr(), block_table.stride(0), self.segments,
-                                     int(block_table.shape[1]), self.max_kv_len, blocks.data_ptr(), s.cuda_stream)
+                                     int(block_table.shape[1]), self.max_kv_len, blocks.data_ptr(),
+                                     ws.data_ptr() if ws is not None else 0, max(0, self.select_bytes), s.cuda_stream)
         return blocks
 
     def run_paged(self, q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor, block_table: torch.Tensor,

@@ -119,18 +119,31 @@ def test_summarize_refusals(bad):
 
 
 def _select(cfg=None, qb=GOOD, n=4, q=GOOD, qs=(1024, 128), tokens=64, sums=GOOD, page=64, pages=9, bt=GOOD, bts=16, segs=2, per_row=16,
-            most=1024, blocks=GOOD):
+            most=1024, blocks=GOOD, ws=GOOD, wsb=1 << 40):
     return B.load().vpp_block_select_paged(ctypes.byref(cfg or _cfg()), qb, n, q, *qs, tokens, sums, page, pages, bt, bts, segs, per_row, most,
-                                           blocks, None)
+                                           blocks, ws, wsb, None)
 
 
 @pytest.mark.parametrize("bad,status", [
     (dict(qb=0), 1), (dict(qb=GOOD + 4), 1), (dict(n=-1), 1), (dict(q=0), 1), (dict(q=GOOD + 8), 1), (dict(qs=(1020, 128)), 1),
     (dict(qs=(1024, 64)), 1), (dict(qs=(64, 128)), 1), (dict(tokens=-1), 1), (dict(sums=0), 1), (dict(sums=GOOD + 2), 1), (dict(page=32), 1),
     (dict(pages=0), 1), (dict(bt=0), 1), (dict(bt=GOOD + 2), 1), (dict(bts=-1), 1), (dict(segs=0), 1), (dict(per_row=0), 1), (dict(most=-1), 1),
-    (dict(blocks=0), 1), (dict(blocks=GOOD + 2), 1), (dict(most=32768 * 64 + 1), 2)])
+    (dict(blocks=0), 1), (dict(blocks=GOOD + 2), 1), (dict(most=32768 * 64 + 1), 2), (dict(ws=0), 3), (dict(ws=GOOD + 64), 3),
+    (dict(wsb=4 * 2 * 16 * 4 - 1), 3)])
 def test_select_refusals(bad, status):
     assert _select(**bad) == status
+
+
+def test_select_workspace():
+    def need(n, most, **over):
+        return B.vpp_block_select_workspace(_cfg(**over), n, most)
+    assert need(4, 1024) == 4 * 2 * 16 * 4 and need(0, 1024) == 0 and need(4, 8 * 64) == 0 and need(4, 8 * 64 + 1) == 4 * 2 * 9 * 4
+    big = need(1 << 20, 1 << 20)
+    assert 255 << 20 < big <= 256 << 20  # a slab, however many query blocks
+    assert need(1 << 20, 1 << 21, num_q_heads=128, num_kv_heads=128) == 64 * 128 * 32768 * 4
+    for args in ((-1, 64), (1, -1), (1, 32768 * 64 + 1)):
+        with pytest.raises(B.VppError):
+            need(*args)
 
 
 def _run(cfg=None, qb=GOOD, n=4, q=GOOD, qs=(1024, 128), tokens=64, k=GOOD, ks=(16384, 256, 128), v=GOOD, vs=(16384, 256, 128), page=64,

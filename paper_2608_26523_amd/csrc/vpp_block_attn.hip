@@ -6,19 +6,30 @@ namespace {
 // ---------------------------------------------------------------------------------------------
 // attention
 // ---------------------------------------------------------------------------------------------
+constexpr int BT = 32;                 // keys of a tile
+constexpr int MAX_PACK = 16;           // query blocks of a workgroup
+constexpr int MAX_ELEMENTS = 1024;     // listed blocks of a workgroup that packs several
+constexpr int MAX_SPLITS = 16;
+// A row's reference maximum moves only when a score passes it by more than 2^LAZY: sums and
+// products share the reference, so quotients do not change, and P stays below 2^LAZY.
+constexpr float LAZY = 8.f;
+
 struct AttendArgs {
     const u16* q;
     const u16* k;
     const u16* v;
     u16* out;
     float* lse;
+    float* part_o;    // [splits][tokens][hq][dv], where the lists are split
+    float* part_lse;  // [splits][tokens][hq], of powers of two
     const vpp_query_block_t* entries;
     const int32_t* lists;
     int64_t q_st, q_sh, k_sp, v_sp, o_st, o_sh, lse_sh;
     int32_t k_st, k_sh, v_st, v_sh;
     Pages pages;
     int32_t num_entries, tokens, segments, query_block, group, hkv;
-    int32_t block_shift, max_blocks, chunks;  // chunks: workgroups that share a query block's rows
+    int32_t block_shift, max_blocks;
+    int32_t pack, rows, chunks, splits;  // query blocks of a workgroup, rows of one; workgroups of their rows, of their lists
     float scale_log2;
 };
 
@@ -37,10 +48,10 @@ __device__ __forceinline__ i32x4 make_rsrc(const void* base, int32_t bytes) {
 // compiler does not wait for it before other LDS reads; the kernel waits itself. The scalar add
 // that sets M0 writes SCC.
 template <int OFF>
-__device__ __forceinline__ void copy16_to_lds(const i32x4& rsrc, uint32_t lds_base, uint32_t voff) {
-    asm volatile("s_add_u32 m0, %0, %3\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
+__device__ __forceinline__ void copy16_to_lds(const i32x4& rsrc, uint32_t lds_base, uint32_t voff, uint32_t soff) {
+    asm volatile("s_add_u32 m0, %0, %3\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %4 offen lds"
                  :
-                 : "s"(lds_base), "v"(voff), "s"(rsrc), "i"(OFF)
+                 : "s"(lds_base), "v"(voff), "s"(rsrc), "i"(OFF), "s"(soff)
                  : "memory", "scc");
 }
 
@@ -62,77 +73,157 @@ __device__ __forceinline__ int vswz(int key, int g) {
     else return g ^ (((key >> 1) & 3) << 1);
 }
 
-// One workgroup takes up to 16 * RB rows -- (token, head) pairs of a query block and a kv head --
-// and each of its waves every fourth tile of 64 listed keys, with all rows: keys and values
-// are read once a workgroup and no wave waits for another until the end, where the four
-// partial results are joined through LDS.
+// A listed block, once for all query blocks of a workgroup that list it.
+struct Element {
+    int key0, page, row;  // position of its first key; its page and first row of it
+    int rows_mask;        // cached rows of it << 16 | query blocks that list it
+};
+
+// The workgroup's tile list. A block that several of its query blocks list becomes one element, with
+// all their bits, if every list ascends (as a selection's do): each block is looked up in the other
+// lists of the same request by bisection, and is left to the first list that has it. Else every
+// entry is an element of its own, so that a block listed twice counts twice.
+__device__ __forceinline__ int list_elements(const AttendArgs& a, const Entry* ents, int entries, int entry0, int head, int* raw,
+                                             Element* elements, int* shared) {
+    const int lane = (int)threadIdx.x & 63, total = entries * a.max_blocks;
+    for (int i = threadIdx.x; i < total; i += NTHREADS) {
+        const int t = i / a.max_blocks, j = i - t * a.max_blocks;
+        const Entry e = ents[t];
+        const int b = a.lists[((int64_t)(entry0 + t) * a.hkv + head) * a.max_blocks + j];
+        raw[i] = e.rows > 0 && b >= 0 && b <= (e.pos0 + e.rows - 1) >> a.block_shift ? b : INT32_MAX;
+    }
+    if (threadIdx.x == 0) shared[0] = 0;
+    __syncthreads();
+    if (entries > 1) {
+        bool bad = false;
+        for (int i = threadIdx.x; i < total; i += NTHREADS)
+            if (i % a.max_blocks && raw[i] <= raw[i - 1] && raw[i - 1] != INT32_MAX) bad = true;
+            else if (i % a.max_blocks && raw[i - 1] == INT32_MAX && raw[i] != INT32_MAX) bad = true;
+        if (__ballot(bad) && lane == 0) shared[0] = 1;
+        __syncthreads();
+    }
+    const bool merge = entries > 1 && shared[0] == 0;
+    auto element = [&](int i, bool& use) {
+        Element x{0, 0, 0, 0};
+        const int b = raw[i];
+        use = b != INT32_MAX;
+        if (!use) return x;
+        const int t = i / a.max_blocks;
+        const Entry e = ents[t];
+        int mask = 1 << t, end = e.pos0 + e.rows;
+        if (merge)
+            for (int o = 0; o < entries; ++o) {
+                const Entry f = ents[o];
+                if (o == t || f.segment != e.segment || f.kv_start != e.kv_start) continue;
+                const int* const r = raw + o * a.max_blocks;
+                int l = 0, h = a.max_blocks;  // first entry >= b
+                while (l < h) {
+                    const int m = (l + h) >> 1;
+                    if (r[m] < b) l = m + 1;
+                    else h = m;
+                }
+                if (l == a.max_blocks || r[l] != b) continue;
+                use = use && o > t;
+                mask |= 1 << o;
+                end = max(end, f.pos0 + f.rows);
+            }
+        x.key0 = b << a.block_shift;
+        const int row = e.kv_start + x.key0;
+        x.page = a.pages.page(e.segment, row);
+        x.row = row & ((1 << a.pages.page_shift) - 1);
+        x.rows_mask = min(1 << a.block_shift, end - x.key0) << 16 | mask;
+        return x;
+    };
+    // compacted in the order of the lists, which is the same every time
+    if (threadIdx.x < 64) {
+        int n = 0;
+        for (int i0 = 0; i0 < total; i0 += 64) {
+            bool use = false;
+            Element x{};
+            if (i0 + lane < total) x = element(i0 + lane, use);
+            const uint64_t all = __ballot(use);
+            if (use) elements[n + count(all & (((uint64_t)1 << lane) - 1))] = x;
+            n += count(all);
+        }
+        if (lane == 0) shared[1] = n;
+    }
+    __syncthreads();
+    return uniform(shared[1]);
+}
+
+// One workgroup takes up to 16 * RB rows -- (token, head) pairs of a kv head, of one query block or
+// of several short ones -- and each of its waves every fourth tile of 32 listed keys, with all rows:
+// keys and values are read once a workgroup and no wave waits for another until the end, where
+// the four partial results are joined through LDS.
 //   S^T = K Q^T on v_mfma_f32_16x16x32_bf16, K straight from memory (16 bytes a lane), Q held in
-//   registers: a lane has one row (column) and 16 of the 64 scores. Softmax in fp32 with exp2.
+//   registers: a lane has one row (column) and 8 of the 32 scores. Softmax in fp32 with exp2.
 //   O^T = V^T P^T: P leaves the scores already as the B operand; V^T is read from an LDS copy of
 //   the row-major tile by ds_read_b64_tr_b16.
+// Infinities and NaN among values that only some rows see would reach the others as 0 * inf. They
+// are not looked for: only if a result is not finite the workgroup does its tiles again, carefully.
 template <int DQK, int DV, int RB>
-__global__ __launch_bounds__(NTHREADS) void attend_kernel(AttendArgs a) {
+__global__ __attribute__((amdgpu_flat_work_group_size(NTHREADS, NTHREADS), amdgpu_waves_per_eu(RB == 1 ? 3 : RB == 2 ? 2 : 1)))
+void attend_kernel(AttendArgs a) {
     constexpr int KS = DQK / 32, DB = DV / 16, VGR = DV / 8;
-    constexpr int V_BYTES = BN * DV * 2, V_LOADS = V_BYTES / 1024;
-    constexpr int ROWS = 16 * RB, OST = DV + 4;  // row stride of a partial result, floats
-    constexpr int BYTES = NWAVES * (2 * V_BYTES > ROWS * OST * 4 ? 2 * V_BYTES : ROWS * OST * 4);
+    constexpr int VB = RB == 1 ? 1 : 2;                    // V buffers of a wave
+    constexpr int V_BYTES = BT * DV * 2, V_LOADS = V_BYTES / 1024;
+    constexpr int ROWS = 16 * RB, JP = RB == 4 ? 2 : 1;    // joined in JP parts of the columns
+    constexpr int OST = DV / JP + 4;                       // row stride of a partial result, floats
+    constexpr int JOIN = NWAVES * ROWS * OST * 4, BYTES = NWAVES * VB * V_BYTES > JOIN ? NWAVES * VB * V_BYTES : JOIN;
     __shared__ __attribute__((aligned(1024))) char smem[BYTES];
-    __shared__ int2 list[MAX_LIST];  // first position and page of the listed blocks
     __shared__ float part_m[NWAVES][ROWS], part_l[NWAVES][ROWS];
-    __shared__ int list_len;
+    __shared__ Entry ents[RB == 1 ? MAX_PACK : 1];
+    __shared__ int shared[4];
+    extern __shared__ Element elements[];  // [pack * max_blocks], and behind them the lists
     const int lane = (int)threadIdx.x & 63, wave = uniform((int)threadIdx.x >> 6);
     const int col = lane & 15, grp = lane >> 4;
 
-    const int head = (int)blockIdx.x % a.hkv, item = (int)blockIdx.x / a.hkv;
-    const int chunk = item % a.chunks, ei = item / a.chunks;
-    const Entry e = uniform(checked_entry(a.entries[ei], a.query_block, a.tokens, a.segments));
-    const int row0 = chunk * ROWS, rows = min(e.rows * a.group - row0, ROWS);  // of the query block's rows
-    if (rows <= 0) return;
-    const int end = e.pos0 + e.rows;  // cached positions of the segment so far
+    const int head = (int)blockIdx.x % a.hkv;
+    int item = (int)blockIdx.x / a.hkv;
+    const int split = item % a.splits;
+    item /= a.splits;
+    const int chunk = item % a.chunks, entry0 = item / a.chunks * a.pack;
+    const int entries = RB == 1 ? min(a.pack, a.num_entries - entry0) : 1;
+    if ((int)threadIdx.x < entries)
+        ents[threadIdx.x] = checked_entry(a.entries[entry0 + threadIdx.x], a.query_block, a.tokens, a.segments);
+    __syncthreads();
+    const int row0 = chunk * ROWS;  // (one query block) of its rows
+    if (entries == 1 && uniform(ents[0].rows) * a.group <= row0) return;
 
-    if (wave == 0) {
-        const int32_t* const from = a.lists + ((int64_t)ei * a.hkv + head) * a.max_blocks;
-        int n = 0;
-        for (int i0 = 0; i0 < a.max_blocks; i0 += 64) {
-            const int b = i0 + lane < a.max_blocks ? from[i0 + lane] : -1;
-            const bool use = b >= 0 && b <= (end - 1) >> a.block_shift;
-            const uint64_t all = __ballot(use);
-            if (use)
-                list[n + count(all & (((uint64_t)1 << lane) - 1))] =
-                    make_int2(b << a.block_shift, a.pages.page(e.segment, e.kv_start + (b << a.block_shift)));
-            n += count(all);
-        }
-        if (lane == 0) list_len = n;
-    }
-
-    // this lane's row of each 16: its token's position, and Q as B operands
+    // this lane's rows: their place, and Q as B operands
     bf16x8 qf[RB][KS];
-    int lim[RB];
+    int lim[RB];  // last position that the row sees
+    int bit = 0;  // of its query block
+    int first_pos = INT32_MAX;
+    for (int t = 0; t < entries; ++t) first_pos = min(first_pos, uniform(ents[t].pos0));
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) {
-        const int r = row0 + min(rb * 16 + col, rows - 1);
+        const int c = row0 + rb * 16 + col, t = RB == 1 ? min(c / a.rows, entries - 1) : 0;
+        const Entry e = ents[t];
+        const int r = max(0, min(c - t * a.rows, e.rows * a.group - 1));  // past the last row: that one again
         const int token = r / a.group, h = head * a.group + r - token * a.group;
         lim[rb] = e.pos0 + token;
+        bit = 1 << t;
         const u16* const p = a.q + (int64_t)(e.row0 + token) * a.q_st + (int64_t)h * a.q_sh + grp * 8;
 #pragma unroll
         for (int s = 0; s < KS; ++s) qf[rb][s] = *(const bf16x8*)(p + s * 32);
     }
-    __syncthreads();
-    const int shift = a.block_shift - 6;  // tiles of a block
-    const int tiles = uniform(list_len) << shift;
+    const int listed = list_elements(a, ents, entries, entry0, head, (int*)(elements + a.pack * a.max_blocks), elements, shared);
+    const int shift = a.block_shift - 5;  // tiles of a block
+    const int tile_end = (int)((int64_t)(listed << shift) * (split + 1) / a.splits);
+    const int tile0 = (int)((int64_t)(listed << shift) * split / a.splits) + wave;
+    const int all_bits = (1 << entries) - 1;
 
     const u16* const kbase = a.k + (int64_t)head * a.k_sh;
     const u16* const vbase = a.v + (int64_t)head * a.v_sh;
-    const int pmask = (1 << a.pages.page_shift) - 1;
-    uint32_t k_off[4], v_src[V_LOADS];
+    const uint32_t k_off = (uint32_t)(col * a.k_st + grp * 8) * 2u;
+    uint32_t v_src[2];  // of the even and of the odd copies of a tile, less what the scalar offset adds
 #pragma unroll
-    for (int kb = 0; kb < 4; ++kb) k_off[kb] = (uint32_t)((kb * 16 + col) * a.k_st + grp * 8) * 2u;
-#pragma unroll
-    for (int t = 0; t < V_LOADS; ++t) {
-        const int key = (t * 64 + lane) / VGR, g = (t * 64 + lane) % VGR;
-        v_src[t] = (uint32_t)(key * a.v_st + vswz<VGR>(key, g) * 8) * 2u;
+    for (int i = 0; i < 2; ++i) {
+        const int key = (i * 64 + lane) / VGR, g = lane % VGR;
+        v_src[i] = (uint32_t)((key - i * (64 / VGR)) * a.v_st + vswz<VGR>(key, g) * 8) * 2u;
     }
-    char* const vbuf = smem + wave * 2 * V_BYTES;
+    char* const vbuf = smem + wave * VB * V_BYTES;
     const uint32_t vbuf_lds = (uint32_t)(uintptr_t)(lds_void_t*)vbuf;
     // V^T: lane group grp reads keys grp * 4 .. + 3 (and 16 further) of 16 columns
     const int tr_key = grp * 4 + (col >> 2);
@@ -141,154 +232,187 @@ __global__ __launch_bounds__(NTHREADS) void attend_kernel(AttendArgs a) {
     for (int d = 0; d < DB; ++d)
         v_at[d] = vbuf_lds + tr_key * (DV * 2) + vswz<VGR>(tr_key, d * 2 + ((col & 3) >> 1)) * 16 + (col & 1) * 8;
 
-    // where tile t's keys are: position of the first, rows of it that are cached, first row's place
-    auto tile = [&](int t, int& key0, int& n, int64_t& page, int& row) {
-        const int2 b = list[t >> shift];
-        key0 = uniform(b.x) + ((t & ((1 << shift) - 1)) << 6);
-        n = max(0, min(BN, end - key0));
-        page = uniform(b.y);
-        row = (e.kv_start + key0) & pmask;
+    struct Tile {
+        int key0, n, page, row, mask;  // n: cached keys of it
     };
-    bf16x8 kf[4][KS];
-    auto load_k = [&](int t) {
-        int key0, n, row;
-        int64_t page;
-        tile(t, key0, n, page, row);
+    auto tile = [&](int t) {
+        const Element x = elements[t >> shift];
+        const int sub = (t & ((1 << shift) - 1)) * BT, rm = uniform(x.rows_mask);
+        return Tile{uniform(x.key0) + sub, max(0, min(BT, (rm >> 16) - sub)), uniform(x.page), uniform(x.row) + sub, rm & 0xffff};
+    };
+    bf16x8 kf[2][KS];
+    auto load_k = [&](const Tile& x) {
         const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(
-            (void*)(kbase + page * a.k_sp + (int64_t)row * a.k_st), 0, (int32_t)((uint32_t)n * (uint32_t)a.k_st * 2u), 0x00020000);
+            (void*)(kbase + x.page * a.k_sp + (int64_t)x.row * a.k_st), 0, (int32_t)((uint32_t)x.n * (uint32_t)a.k_st * 2u), 0x00020000);
 #pragma unroll
-        for (int kb = 0; kb < 4; ++kb)
+        for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
             for (int s = 0; s < KS; ++s)
-                kf[kb][s] = __builtin_bit_cast(bf16x8, __builtin_amdgcn_raw_buffer_load_b128(r, (int)k_off[kb] + s * 64, 0, 0));
+                kf[kb][s] = __builtin_bit_cast(bf16x8, __builtin_amdgcn_raw_buffer_load_b128(r, (int)k_off + s * 64, kb * 32 * a.k_st, 0));
     };
-    auto copy_v = [&](int t, int buf) {
-        int key0, n, row;
-        int64_t page;
-        tile(t, key0, n, page, row);
-        const i32x4 r = make_rsrc(vbase + page * a.v_sp + (int64_t)row * a.v_st, (int32_t)((uint32_t)n * (uint32_t)a.v_st * 2u));
-        static_for<V_LOADS>([&](auto T) { copy16_to_lds<decltype(T)::value * 1024>(r, vbuf_lds + buf * V_BYTES, v_src[decltype(T)::value]); });
+    auto copy_v = [&](const Tile& x, int buf) {
+        const i32x4 r = make_rsrc(vbase + x.page * a.v_sp + (int64_t)x.row * a.v_st, (int32_t)((uint32_t)x.n * (uint32_t)a.v_st * 2u));
+        static_for<V_LOADS>([&](auto T) {
+            constexpr int t = decltype(T)::value;
+            copy16_to_lds<t * 1024>(r, vbuf_lds + buf * V_BYTES, v_src[t % 2], (uint32_t)(t * (64 / VGR) * 2) * (uint32_t)a.v_st);
+        });
     };
 
     float m_run[RB], l_run[RB];  // the row's reference maximum; this lane's share of its sum
     f32x4 o[RB][DB];
-#pragma unroll
-    for (int rb = 0; rb < RB; ++rb) {
-        m_run[rb] = -INFINITY;
-        l_run[rb] = 0;
-#pragma unroll
-        for (int d = 0; d < DB; ++d) o[rb][d] = f32x4{0, 0, 0, 0};
-    }
-    if (wave < tiles) {
-        copy_v(wave, 0);
-        load_k(wave);
-    }
-    int buf = 0;
-    for (int t = wave; t < tiles; t += NWAVES, buf ^= 1) {
-        int key0, n, row;
-        int64_t page;
-        tile(t, key0, n, page, row);
-        f32x4 s[RB][4];
-#pragma unroll
-        for (int kb = 0; kb < 4; ++kb)
-#pragma unroll
-            for (int rb = 0; rb < RB; ++rb) {
-                s[rb][kb] = f32x4{0, 0, 0, 0};
-#pragma unroll
-                for (int k = 0; k < KS; ++k)
-                    s[rb][kb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[kb][k], qf[rb][k], s[rb][kb], 0, 0, 0);
-            }
-        // this tile's values are in LDS once the loads up to here are done, and the other buffer is
-        // free once the last tile's reads of it are
-        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
-        if (t + NWAVES < tiles) {
-            copy_v(t + NWAVES, buf ^ 1);
-            load_k(t + NWAVES);
-        }
-        const bool masked = key0 + BN - 1 > e.pos0;
-        // Values of keys that not every row sees would reach the others as 0 * inf: here they
-        // count as 0, and the rows that see them get them after the product.
-        uint64_t wild = 0;
-        if (masked && e.rows > 1) {
-            bool any = false;
-#pragma unroll 1
-            for (int i = 0; i < V_LOADS; ++i) {
-                const int key = (i * 64 + lane) / VGR;
-                if (key0 + key <= e.pos0) continue;
-                u32x4* const at = (u32x4*)(vbuf + buf * V_BYTES + (i * 64 + lane) * 16);
-                u32x4 x = *at;
-                bool bad = false;
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    if ((x[j] & 0x7f80u) == 0x7f80u) x[j] &= 0xffff0000u, bad = true;
-                    if ((x[j] & 0x7f800000u) == 0x7f800000u) x[j] &= 0xffffu, bad = true;
-                }
-                if (bad) *at = x;
-                any = any || bad;
-            }
-            wild = __ballot(any);
-        }
-        bf16x8 p[RB][2];
+    for (bool careful = false;; careful = true) {
 #pragma unroll
         for (int rb = 0; rb < RB; ++rb) {
-            if (masked) {
+            m_run[rb] = -INFINITY;
+            l_run[rb] = 0;
 #pragma unroll
-                for (int kb = 0; kb < 4; ++kb)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        if (key0 + kb * 16 + grp * 4 + i > lim[rb]) s[rb][kb][i] = -INFINITY;
-            }
-            float top = -INFINITY;
-#pragma unroll
-            for (int kb = 0; kb < 4; ++kb)
-                top = fmaxf(top, fmaxf(fmaxf(s[rb][kb][0], s[rb][kb][1]), fmaxf(s[rb][kb][2], s[rb][kb][3])));
-            top = max_xor32(max_xor16(top)) * a.scale_log2;
-            const float m = fmaxf(m_run[rb], top);
-            const float use = m == -INFINITY ? 0.f : m;
-            const float alpha = __builtin_amdgcn_exp2f(m_run[rb] - use);
-            m_run[rb] = m;
-            float sum = 0;
-#pragma unroll
-            for (int kb = 0; kb < 4; ++kb)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[rb][kb][i], a.scale_log2, -use));
-                    sum += x;
-                    p[rb][kb / 2][kb % 2 * 4 + i] = (__bf16)x;
-                }
-            l_run[rb] = l_run[rb] * alpha + sum;
-#pragma unroll
-            for (int d = 0; d < DB; ++d) o[rb][d] *= alpha;
+            for (int d = 0; d < DB; ++d) o[rb][d] = f32x4{0, 0, 0, 0};
         }
+        int buf = 0;
+        Tile now{}, next{};
+        if (tile0 < tile_end) {
+            now = tile(tile0);
+            copy_v(now, 0);
+            load_k(now);
+        }
+        for (int t = tile0; t < tile_end; t += NWAVES, now = next) {
+            f32x4 s[RB][2];
 #pragma unroll
-        for (int kk = 0; kk < 2; ++kk)
+            for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                for (int rb = 0; rb < RB; ++rb) {
+                    s[rb][kb] = f32x4{0, 0, 0, 0};
+#pragma unroll
+                    for (int k = 0; k < KS; ++k)
+                        s[rb][kb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[kb][k], qf[rb][k], s[rb][kb], 0, 0, 0);
+                }
+            const bool more = t + NWAVES < tile_end;
+            if (more) next = tile(t + NWAVES);
+            if constexpr (VB == 2) {
+                // this tile's values are in LDS once the loads up to here are done, and the other buffer is
+                // free once the last tile's reads of it are
+                asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+                if (more) copy_v(next, buf ^ 1);
+            }
+            if (more) load_k(next);
+            const bool masked = now.key0 + BT - 1 > first_pos, partial = now.mask != all_bits;
+            if (masked || partial) {
+#pragma unroll
+                for (int rb = 0; rb < RB; ++rb) {
+                    const int last = now.mask & bit ? lim[rb] : -1;
+#pragma unroll
+                    for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            if (now.key0 + kb * 16 + grp * 4 + i > last) s[rb][kb][i] = -INFINITY;
+                }
+            }
+            bool above = false;
+            float top[RB];
+#pragma unroll
+            for (int rb = 0; rb < RB; ++rb) {
+                top[rb] = fmaxf(fmaxf(fmaxf(s[rb][0][0], s[rb][0][1]), fmaxf(s[rb][0][2], s[rb][0][3])),
+                                fmaxf(fmaxf(s[rb][1][0], s[rb][1][1]), fmaxf(s[rb][1][2], s[rb][1][3]))) * a.scale_log2;
+                above = above || top[rb] > m_run[rb] + LAZY;
+            }
+            if (__ballot(above)) {
+#pragma unroll
+                for (int rb = 0; rb < RB; ++rb) {
+                    const float m = fmaxf(m_run[rb], max_xor32(max_xor16(top[rb])));
+                    const float alpha = __builtin_amdgcn_exp2f(m_run[rb] - (m == -INFINITY ? 0.f : m));
+                    m_run[rb] = m;
+                    l_run[rb] *= alpha;
+#pragma unroll
+                    for (int d = 0; d < DB; ++d) o[rb][d] *= alpha;
+                }
+            }
+            bf16x8 p[RB];
+#pragma unroll
+            for (int rb = 0; rb < RB; ++rb) {
+                const float use = m_run[rb] == -INFINITY ? 0.f : m_run[rb];
+#pragma unroll
+                for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[rb][kb][i], a.scale_log2, -use));
+                        l_run[rb] += x;
+                        p[rb][kb * 4 + i] = (__bf16)x;
+                    }
+            }
+            if constexpr (VB == 1) {
+                // this tile's values are in LDS: only the keys of the next one are younger
+                if (more) asm volatile("s_waitcnt vmcnt(%0)" ::"i"(2 * KS) : "memory");
+                else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            }
+            bool wild = false;
+            if (careful && (masked || partial)) {
+                // values that are not finite count as 0 here; the rows that see them get them after the product
+#pragma unroll 1
+                for (int i = 0; i < V_LOADS; ++i) {
+                    u32x4* const at = (u32x4*)(vbuf + buf * V_BYTES + (i * 64 + lane) * 16);
+                    u32x4 x = *at;
+                    bool bad = false;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        if ((x[j] & 0x7f80u) == 0x7f80u) x[j] &= 0xffff0000u, bad = true;
+                        if ((x[j] & 0x7f800000u) == 0x7f800000u) x[j] &= 0xffffu, bad = true;
+                    }
+                    if (bad) *at = x;
+                    wild = wild || bad;
+                }
+                wild = __ballot(wild) != 0;
+            }
 #pragma unroll
             for (int d = 0; d < DB; ++d) {
-                const uint32_t at = v_at[d] + buf * V_BYTES + kk * 32 * DV * 2;
+                const uint32_t at = v_at[d] + buf * V_BYTES;
                 const i16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4*)(uintptr_t)at);
                 const i16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4*)(uintptr_t)(at + 16 * DV * 2));
                 bf16x8 vf;
                 __builtin_memcpy(&vf, &x, 8);
                 __builtin_memcpy((char*)&vf + 8, &y, 8);
 #pragma unroll
-                for (int rb = 0; rb < RB; ++rb) o[rb][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, p[rb][kk], o[rb][d], 0, 0, 0);
+                for (int rb = 0; rb < RB; ++rb) o[rb][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, p[rb], o[rb][d], 0, 0, 0);
             }
-        if (wild) {
-            const u16* const v0 = vbase + page * a.v_sp + (int64_t)row * a.v_st + grp * 4;
+            if (wild) {
+                const u16* const v0 = vbase + now.page * a.v_sp + (int64_t)now.row * a.v_st + grp * 4;
 #pragma unroll 1
-            for (int key = max(0, e.pos0 + 1 - key0); key < n; ++key)
+                for (int key = 0; key < now.n; ++key)
 #pragma unroll
-                for (int d = 0; d < DB; ++d) {
-                    const u32x2 x = *(const u32x2*)(v0 + (int64_t)key * a.v_st + d * 16);
+                    for (int d = 0; d < DB; ++d) {
+                        const u32x2 x = *(const u32x2*)(v0 + (int64_t)key * a.v_st + d * 16);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const float v = __uint_as_float(i % 2 ? x[i / 2] & 0xffff0000u : x[i / 2] << 16);
+                        for (int i = 0; i < 4; ++i) {
+                            const float v = __uint_as_float(i % 2 ? x[i / 2] & 0xffff0000u : x[i / 2] << 16);
 #pragma unroll
-                        for (int rb = 0; rb < RB; ++rb)
-                            if (!(fabsf(v) < INFINITY) && key0 + key <= lim[rb]) o[rb][d][i] += v;
+                            for (int rb = 0; rb < RB; ++rb)
+                                if (!(fabsf(v) < INFINITY) && now.key0 + key <= (now.mask & bit ? lim[rb] : -1)) o[rb][d][i] += v;
+                        }
                     }
+            }
+            if constexpr (VB == 1) {
+                // the buffer is free once the reads above are done
+                if (more) {
+                    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+                    copy_v(next, 0);
                 }
+            } else {
+                buf ^= 1;
+            }
         }
+        // 0 * inf is NaN
+        float probe = 0;
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+            for (int d = 0; d < DB; ++d)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) probe = __builtin_fmaf(o[rb][d][i], 0.f, probe);
+        if (threadIdx.x == 0) shared[2] = 0;
+        __syncthreads();  // every wave is past its last tile: smem is free
+        if (__ballot(probe != 0) && lane == 0) shared[2] = 1;
+        __syncthreads();
+        if (careful || uniform(shared[2]) == 0) break;
+        __syncthreads();
     }
 
     // join the waves' partial results
@@ -300,37 +424,105 @@ __global__ __launch_bounds__(NTHREADS) void attend_kernel(AttendArgs a) {
             part_l[wave][rb * 16 + col] = l;
         }
     }
-    __syncthreads();  // every wave is past its last tile: smem is free
     float* const part = (float*)smem;
 #pragma unroll
-    for (int rb = 0; rb < RB; ++rb)
+    for (int jp = 0; jp < JP; ++jp) {
+        if (jp > 0) __syncthreads();
 #pragma unroll
-        for (int d = 0; d < DB; ++d)
-            *(f32x4*)(part + (wave * ROWS + rb * 16 + col) * OST + d * 16 + grp * 4) = o[rb][d];
-    __syncthreads();
-    for (int i = threadIdx.x; i < rows * (DV / 8); i += NTHREADS) {
-        const int r = i / (DV / 8), g = i % (DV / 8);
-        float m = part_m[0][r];
+        for (int rb = 0; rb < RB; ++rb)
 #pragma unroll
-        for (int w = 1; w < NWAVES; ++w) m = fmaxf(m, part_m[w][r]);
+            for (int d = 0; d < DB / JP; ++d)
+                *(f32x4*)(part + (wave * ROWS + rb * 16 + col) * OST + d * 16 + grp * 4) = o[rb][jp * (DB / JP) + d];
+        __syncthreads();
+        constexpr int GR = DV / 8 / JP;  // granules of a row of this part
+        for (int i = threadIdx.x; i < ROWS * GR; i += NTHREADS) {
+            const int c = i / GR, g = i % GR;
+            const int t = RB == 1 ? min((row0 + c) / a.rows, entries - 1) : 0;
+            const Entry e = ents[t];
+            const int r = row0 + c - t * a.rows;
+            if (r >= e.rows * a.group) continue;
+            float m = part_m[0][c];
+#pragma unroll
+            for (int w = 1; w < NWAVES; ++w) m = fmaxf(m, part_m[w][c]);
+            const float use = m == -INFINITY ? 0.f : m;
+            float l = 0, x[8] = {};
+#pragma unroll
+            for (int w = 0; w < NWAVES; ++w) {
+                const float f = __builtin_amdgcn_exp2f(part_m[w][c] - use);
+                l += part_l[w][c] * f;
+                const float* const y = part + (w * ROWS + c) * OST + g * 8;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) x[j] += y[j] * f;
+            }
+            const float inv = l > 0 ? 1 / l : l;  // no key: zeros
+            const int token = e.row0 + r / a.group, h = head * a.group + r % a.group, at = (jp * GR + g) * 8;
+            const float lse = l > 0 ? m + __builtin_amdgcn_logf(l) : l == 0 ? -INFINITY : l;
+            if (a.splits > 1) {
+                const int64_t i0 = ((int64_t)split * a.tokens + token) * (a.group * a.hkv) + h;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) a.part_o[i0 * DV + at + j] = x[j] * inv;
+                if (at == 0) a.part_lse[i0] = lse;
+                continue;
+            }
+            bf16x8 res;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) res[j] = (__bf16)(x[j] * inv);
+            *(bf16x8*)(a.out + (int64_t)token * a.o_st + (int64_t)h * a.o_sh + at) = res;
+            if (at == 0 && a.lse) a.lse[(int64_t)h * a.lse_sh + token] = lse * LN2;
+        }
+    }
+}
+
+// The parts of split lists, weighted by their sums: a thread 8 values of a row. Rows of no query
+// block stay as they are.
+template <int DV>
+__global__ __launch_bounds__(NTHREADS) void merge_kernel(AttendArgs a) {
+    constexpr int GR = DV / 8;
+    const int hq = a.group * a.hkv;
+    const Entry e = uniform(checked_entry(a.entries[blockIdx.x], a.query_block, a.tokens, a.segments));
+    for (int i = (int)blockIdx.y * NTHREADS + (int)threadIdx.x; i < e.rows * hq * GR; i += (int)gridDim.y * NTHREADS) {
+        const int g = i % GR, h = i / GR % hq, token = e.row0 + i / GR / hq;
+        const int64_t i0 = (int64_t)token * hq + h, st = (int64_t)a.tokens * hq;
+        float m = a.part_lse[i0];
+        for (int s = 1; s < a.splits; ++s) m = fmaxf(m, a.part_lse[i0 + s * st]);
         const float use = m == -INFINITY ? 0.f : m;
         float l = 0, x[8] = {};
+        for (int s = 0; s < a.splits; ++s) {
+            const float f = __builtin_amdgcn_exp2f(a.part_lse[i0 + s * st] - use);
+            l += f;
+            const float* const y = a.part_o + (i0 + s * st) * DV + g * 8;
 #pragma unroll
-        for (int w = 0; w < NWAVES; ++w) {
-            const float f = __builtin_amdgcn_exp2f(part_m[w][r] - use);
-            l += part_l[w][r] * f;
-            const float* const y = part + (w * ROWS + r) * OST + g * 8;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) x[j] += y[j] * f;
+            for (int j = 0; j < 8; ++j) x[j] += f > 0 || f != f ? y[j] * f : 0;
         }
-        const float inv = l > 0 ? 1 / l : l;  // no key: zeros
+        const float inv = l > 0 ? 1 / l : l;
         bf16x8 res;
 #pragma unroll
         for (int j = 0; j < 8; ++j) res[j] = (__bf16)(x[j] * inv);
-        const int tl = (row0 + r) / a.group, h = head * a.group + (row0 + r) % a.group;
-        *(bf16x8*)(a.out + (int64_t)(e.row0 + tl) * a.o_st + (int64_t)h * a.o_sh + g * 8) = res;
-        if (g == 0 && a.lse) a.lse[(int64_t)h * a.lse_sh + e.row0 + tl] = l > 0 ? (m + __builtin_amdgcn_logf(l)) * LN2 : l == 0 ? -INFINITY : l;
+        *(bf16x8*)(a.out + (int64_t)token * a.o_st + (int64_t)h * a.o_sh + g * 8) = res;
+        if (g == 0 && a.lse) a.lse[(int64_t)h * a.lse_sh + token] = (l > 0 ? m + __builtin_amdgcn_logf(l) : l == 0 ? -INFINITY : l) * LN2;
     }
+}
+
+// How a launch is cut up: query blocks of a workgroup, workgroups of a query block's rows, parts of the lists.
+struct Cut {
+    int rb, rows, pack, chunks, splits;
+};
+Cut cut_of(const vpp_block_attn_config_t& c, int64_t num_query_blocks) {
+    Cut u;
+    u.rows = c.num_q_heads / c.num_kv_heads * c.query_block;
+    u.rb = u.rows <= 16 ? 1 : u.rows <= 32 ? 2 : 4;
+    u.chunks = (u.rows + 16 * u.rb - 1) / (16 * u.rb);
+    // Several query blocks share a workgroup's 16 columns, and the blocks that they list in common, while
+    // there are four workgroups a CU left.
+    u.pack = u.rows <= 16 ? 16 / u.rows : 1;
+    while (u.pack > 1 && (u.pack * c.max_blocks > MAX_ELEMENTS || num_query_blocks * c.num_kv_heads / u.pack < 1024)) u.pack /= 2;
+    // Few workgroups split their lists, down to two tiles a wave.
+    const int64_t wgs = (num_query_blocks + u.pack - 1) / u.pack * u.chunks * c.num_kv_heads;
+    const int64_t tiles = (int64_t)c.max_blocks * (c.block_size / BT), most = tiles / (2 * NWAVES);
+    int64_t s = wgs > 0 && wgs < 256 ? (512 + wgs - 1) / wgs : 1;
+    if (s > most) s = most;
+    u.splits = (int)(s < 1 ? 1 : s > MAX_SPLITS ? MAX_SPLITS : s);
+    return u;
 }
 
 }  // namespace
@@ -340,7 +532,8 @@ extern "C" vpp_status_t vpp_block_attn_workspace(const vpp_block_attn_config_t* 
     const vpp_status_t st = check_config(cfg);
     if (st != VPP_OK) return st;
     if (num_query_blocks < 0 || num_tokens < 0 || !bytes) return VPP_ERR_INVALID_ARG;
-    *bytes = 0;
+    const int splits = cut_of(*cfg, num_query_blocks).splits;
+    *bytes = splits > 1 ? (size_t)splits * num_tokens * cfg->num_q_heads * (cfg->head_dim_v + 1) * 4 : 0;
     return VPP_OK;
 }
 
@@ -395,14 +588,28 @@ extern "C" vpp_status_t vpp_block_attn_run_paged(
     a.block_shift = log2_of(cfg->block_size);
     a.max_blocks = cfg->max_blocks;
     a.scale_log2 = (cfg->softmax_scale > 0 ? cfg->softmax_scale : 1 / sqrtf((float)cfg->head_dim_qk)) * LOG2E;
-    const int rows = a.group * a.query_block, rb = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
-    a.chunks = (rows + 16 * rb - 1) / (16 * rb);
-    const int64_t grid = (int64_t)num_query_blocks * a.chunks * hkv;
+    const Cut cut = cut_of(*cfg, num_query_blocks);
+    a.pack = cut.pack;
+    a.rows = cut.rows;
+    a.chunks = cut.chunks;
+    a.splits = cut.splits;
+    if (a.splits > 1) {
+        const size_t need = (size_t)a.splits * num_tokens * hq * (dv + 1) * 4;
+        if (!workspace || ((uintptr_t)workspace & 255u) || workspace_bytes < need) return VPP_ERR_WORKSPACE;
+        a.part_o = (float*)workspace;
+        a.part_lse = a.part_o + (size_t)a.splits * num_tokens * hq * dv;
+    }
+    const int64_t grid = (int64_t)((num_query_blocks + a.pack - 1) / a.pack) * a.chunks * a.splits * hkv;
     if (grid >= ((int64_t)1 << 31)) return VPP_ERR_INVALID_ARG;
-    (void)workspace;
-    (void)workspace_bytes;
-    auto* kernel = cfg->head_dim_qk == 64 ? pick_attend<64, 64>(rb)
-                   : cfg->head_dim_qk == 128 ? pick_attend<128, 128>(rb) : pick_attend<192, 128>(rb);
-    hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(NTHREADS), 0, (hipStream_t)stream, a);
-    return hipGetLastError() == hipSuccess ? VPP_OK : VPP_ERR_HIP;
+    const size_t lds = (size_t)a.pack * a.max_blocks * (sizeof(Element) + 4);
+    auto* kernel = dqk == 64 ? pick_attend<64, 64>(cut.rb) : dqk == 128 ? pick_attend<128, 128>(cut.rb) : pick_attend<192, 128>(cut.rb);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(NTHREADS), lds, (hipStream_t)stream, a);
+    if (hipGetLastError() != hipSuccess) return VPP_ERR_HIP;
+    if (a.splits > 1) {
+        const int per = cfg->query_block * hq * (dv / 8), y = (per + NTHREADS - 1) / NTHREADS;
+        auto* merge = dv == 64 ? merge_kernel<64> : merge_kernel<128>;
+        hipLaunchKernelGGL(merge, dim3((unsigned)num_query_blocks, (unsigned)(y < 256 ? y : 256)), dim3(NTHREADS), 0, (hipStream_t)stream, a);
+        if (hipGetLastError() != hipSuccess) return VPP_ERR_HIP;
+    }
+    return VPP_OK;
 }

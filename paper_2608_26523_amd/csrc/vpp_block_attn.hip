@@ -8,7 +8,7 @@ namespace {
 // ---------------------------------------------------------------------------------------------
 constexpr int BT = 32;                 // keys of a tile
 constexpr int MAX_PACK = 16;           // query blocks of a workgroup
-constexpr int MAX_ELEMENTS = 1024;     // listed blocks of a workgroup that packs several
+constexpr int MAX_ELEMENTS = 2048;     // listed blocks of a workgroup that packs several
 constexpr int MAX_SPLITS = 16;
 // A row's reference maximum moves only when a score passes it by more than 2^LAZY: sums and
 // products share the reference, so quotients do not change, and P stays below 2^LAZY.
@@ -64,6 +64,14 @@ __device__ __forceinline__ void static_for(F&& f) {
     static_for_impl(f, std::make_integer_sequence<int, N>());
 }
 
+// Granule of a K row that sits at granule g of its LDS row. ds_read_b128 serves 16 lanes at once, here one
+// granule of 16 rows: they must fall on different 16-byte parts of the banks' 256 bytes.
+template <int KGR>
+__device__ __forceinline__ int kswz(int row, int g) {
+    if constexpr (KGR % 16 == 0) return g ^ (row & 15);
+    else return g ^ ((row >> 1) & 7);
+}
+
 // Granule of a V row that sits at granule g of its LDS row. ds_read_b64_tr_b16 serves 32 lanes at
 // once, here 8 consecutive keys x 32 bytes: those 8 must fall on different 32-byte parts of the
 // 256 bytes that the banks serve.
@@ -103,16 +111,12 @@ __device__ __forceinline__ int list_elements(const AttendArgs& a, const Entry* e
         __syncthreads();
     }
     const bool merge = entries > 1 && shared[0] == 0;
-    auto element = [&](int i, bool& use) {
-        Element x{0, 0, 0, 0};
-        const int b = raw[i];
-        use = b != INT32_MAX;
-        if (!use) return x;
-        const int t = i / a.max_blocks;
+    for (int i = threadIdx.x; i < total; i += NTHREADS) {
+        const int b = raw[i], t = i / a.max_blocks;
         const Entry e = ents[t];
-        int mask = 1 << t, end = e.pos0 + e.rows;
-        if (merge)
-            for (int o = 0; o < entries; ++o) {
+        int mask = b == INT32_MAX ? 0 : 1 << t, end = e.pos0 + e.rows;
+        if (merge && mask)
+            for (int o = 0; o < entries && mask; ++o) {
                 const Entry f = ents[o];
                 if (o == t || f.segment != e.segment || f.kv_start != e.kv_start) continue;
                 const int* const r = raw + o * a.max_blocks;
@@ -123,24 +127,27 @@ __device__ __forceinline__ int list_elements(const AttendArgs& a, const Entry* e
                     else h = m;
                 }
                 if (l == a.max_blocks || r[l] != b) continue;
-                use = use && o > t;
-                mask |= 1 << o;
+                mask = o < t ? 0 : mask | 1 << o;
                 end = max(end, f.pos0 + f.rows);
             }
-        x.key0 = b << a.block_shift;
-        const int row = e.kv_start + x.key0;
-        x.page = a.pages.page(e.segment, row);
-        x.row = row & ((1 << a.pages.page_shift) - 1);
-        x.rows_mask = min(1 << a.block_shift, end - x.key0) << 16 | mask;
-        return x;
-    };
-    // compacted in the order of the lists, which is the same every time
+        Element x{0, 0, 0, 0};
+        if (mask) {
+            x.key0 = b << a.block_shift;
+            const int row = e.kv_start + x.key0;
+            x.page = a.pages.page(e.segment, row);
+            x.row = row & ((1 << a.pages.page_shift) - 1);
+            x.rows_mask = min(1 << a.block_shift, end - x.key0) << 16 | mask;
+        }
+        elements[i] = x;
+    }
+    __syncthreads();
+    // compacted in the order of the lists, which is the same every time; a wave reads 64 before it writes
     if (threadIdx.x < 64) {
         int n = 0;
         for (int i0 = 0; i0 < total; i0 += 64) {
-            bool use = false;
-            Element x{};
-            if (i0 + lane < total) x = element(i0 + lane, use);
+            Element x{0, 0, 0, 0};
+            if (i0 + lane < total) x = elements[i0 + lane];
+            const bool use = (x.rows_mask & 0xffff) != 0;
             const uint64_t all = __ballot(use);
             if (use) elements[n + count(all & (((uint64_t)1 << lane) - 1))] = x;
             n += count(all);
@@ -161,18 +168,22 @@ __device__ __forceinline__ int list_elements(const AttendArgs& a, const Entry* e
 //   the row-major tile by ds_read_b64_tr_b16.
 // Infinities and NaN among values that only some rows see would reach the others as 0 * inf. They
 // are not looked for: only if a result is not finite the workgroup does its tiles again, carefully.
-template <int DQK, int DV, int RB>
+// SKIP: several query blocks, and tiles that none of a 16 rows' lists pass them by.
+template <int DQK, int DV, int RB, bool SKIP>
 __global__ __attribute__((amdgpu_flat_work_group_size(NTHREADS, NTHREADS), amdgpu_waves_per_eu(RB == 1 ? 3 : RB == 2 ? 2 : 1)))
 void attend_kernel(AttendArgs a) {
-    constexpr int KS = DQK / 32, DB = DV / 16, VGR = DV / 8;
-    constexpr int VB = RB == 1 ? 1 : 2;                    // V buffers of a wave
-    constexpr int V_BYTES = BT * DV * 2, V_LOADS = V_BYTES / 1024;
+    constexpr int KS = DQK / 32, DB = DV / 16, KGR = DQK / 8, VGR = DV / 8;
+    constexpr int K_BYTES = BT * DQK * 2, K_LOADS = K_BYTES / 1024, V_BYTES = BT * DV * 2, V_LOADS = V_BYTES / 1024;
+    constexpr int VB = RB == 4 ? 2 : 1;                    // V buffers of a wave
+    constexpr int WAVE_BYTES = K_BYTES + VB * V_BYTES;
+    // copies of a tile after which the swizzle repeats
+    constexpr int K_PERIOD = KGR == 16 ? 4 : KGR == 24 ? 6 : 2;
     constexpr int ROWS = 16 * RB, JP = RB == 4 ? 2 : 1;    // joined in JP parts of the columns
     constexpr int OST = DV / JP + 4;                       // row stride of a partial result, floats
-    constexpr int JOIN = NWAVES * ROWS * OST * 4, BYTES = NWAVES * VB * V_BYTES > JOIN ? NWAVES * VB * V_BYTES : JOIN;
+    constexpr int JOIN = NWAVES * ROWS * OST * 4, BYTES = NWAVES * WAVE_BYTES > JOIN ? NWAVES * WAVE_BYTES : JOIN;
     __shared__ __attribute__((aligned(1024))) char smem[BYTES];
     __shared__ float part_m[NWAVES][ROWS], part_l[NWAVES][ROWS];
-    __shared__ Entry ents[RB == 1 ? MAX_PACK : 1];
+    __shared__ Entry ents[MAX_PACK];
     __shared__ int shared[4];
     extern __shared__ Element elements[];  // [pack * max_blocks], and behind them the lists
     const int lane = (int)threadIdx.x & 63, wave = uniform((int)threadIdx.x >> 6);
@@ -183,7 +194,7 @@ void attend_kernel(AttendArgs a) {
     const int split = item % a.splits;
     item /= a.splits;
     const int chunk = item % a.chunks, entry0 = item / a.chunks * a.pack;
-    const int entries = RB == 1 ? min(a.pack, a.num_entries - entry0) : 1;
+    const int entries = min(a.pack, a.num_entries - entry0);
     if ((int)threadIdx.x < entries)
         ents[threadIdx.x] = checked_entry(a.entries[entry0 + threadIdx.x], a.query_block, a.tokens, a.segments);
     __syncthreads();
@@ -192,18 +203,21 @@ void attend_kernel(AttendArgs a) {
 
     // this lane's rows: their place, and Q as B operands
     bf16x8 qf[RB][KS];
-    int lim[RB];  // last position that the row sees
-    int bit = 0;  // of its query block
+    int lim[RB], bit[RB];  // last position that the row sees; its query block's bit
+    int bits[RB];          // of the query blocks of these 16 rows
     int first_pos = INT32_MAX;
     for (int t = 0; t < entries; ++t) first_pos = min(first_pos, uniform(ents[t].pos0));
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) {
-        const int c = row0 + rb * 16 + col, t = RB == 1 ? min(c / a.rows, entries - 1) : 0;
+        const int c = row0 + rb * 16 + col, t = entries > 1 ? min(c / a.rows, entries - 1) : 0;
         const Entry e = ents[t];
         const int r = max(0, min(c - t * a.rows, e.rows * a.group - 1));  // past the last row: that one again
         const int token = r / a.group, h = head * a.group + r - token * a.group;
         lim[rb] = e.pos0 + token;
-        bit = 1 << t;
+        bit[rb] = 1 << t;
+        // (none of its own: those of the last, which the tiles do anyway)
+        const int t0 = entries > 1 ? min(rb * 16 / a.rows, entries - 1) : 0, t1 = entries > 1 ? min((rb * 16 + 15) / a.rows, entries - 1) : 0;
+        bits[rb] = (2 << t1) - (1 << t0);
         const u16* const p = a.q + (int64_t)(e.row0 + token) * a.q_st + (int64_t)h * a.q_sh + grp * 8;
 #pragma unroll
         for (int s = 0; s < KS; ++s) qf[rb][s] = *(const bf16x8*)(p + s * 32);
@@ -216,15 +230,24 @@ void attend_kernel(AttendArgs a) {
 
     const u16* const kbase = a.k + (int64_t)head * a.k_sh;
     const u16* const vbase = a.v + (int64_t)head * a.v_sh;
-    const uint32_t k_off = (uint32_t)(col * a.k_st + grp * 8) * 2u;
-    uint32_t v_src[2];  // of the even and of the odd copies of a tile, less what the scalar offset adds
+    // sources of a tile's copies, less what the scalar offset adds
+    uint32_t k_src[K_PERIOD], v_src[2];
+#pragma unroll
+    for (int i = 0; i < K_PERIOD; ++i) {
+        const int slot = i * 64 + lane, key = slot / KGR, g = slot % KGR;
+        k_src[i] = (uint32_t)(key * a.k_st + kswz<KGR>(key, g) * 8) * 2u;
+    }
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-        const int key = (i * 64 + lane) / VGR, g = lane % VGR;
-        v_src[i] = (uint32_t)((key - i * (64 / VGR)) * a.v_st + vswz<VGR>(key, g) * 8) * 2u;
+        const int slot = i * 64 + lane, key = slot / VGR, g = slot % VGR;
+        v_src[i] = (uint32_t)(key * a.v_st + vswz<VGR>(key, g) * 8) * 2u;
     }
-    char* const vbuf = smem + wave * VB * V_BYTES;
-    const uint32_t vbuf_lds = (uint32_t)(uintptr_t)(lds_void_t*)vbuf;
+    char* const vbuf = smem + wave * WAVE_BYTES;
+    const uint32_t vbuf_lds = (uint32_t)(uintptr_t)(lds_void_t*)vbuf, kbuf_lds = vbuf_lds + VB * V_BYTES;
+    // K: lane group grp reads granule 4 s + grp of row col (and of the row 16 further)
+    const u32x4* k_at[KS];
+#pragma unroll
+    for (int s = 0; s < KS; ++s) k_at[s] = (const u32x4*)(vbuf + VB * V_BYTES + col * (DQK * 2) + kswz<KGR>(col, s * 4 + grp) * 16);
     // V^T: lane group grp reads keys grp * 4 .. + 3 (and 16 further) of 16 columns
     const int tr_key = grp * 4 + (col >> 2);
     uint32_t v_at[DB];
@@ -240,21 +263,18 @@ void attend_kernel(AttendArgs a) {
         const int sub = (t & ((1 << shift) - 1)) * BT, rm = uniform(x.rows_mask);
         return Tile{uniform(x.key0) + sub, max(0, min(BT, (rm >> 16) - sub)), uniform(x.page), uniform(x.row) + sub, rm & 0xffff};
     };
-    bf16x8 kf[2][KS];
-    auto load_k = [&](const Tile& x) {
-        const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(
-            (void*)(kbase + x.page * a.k_sp + (int64_t)x.row * a.k_st), 0, (int32_t)((uint32_t)x.n * (uint32_t)a.k_st * 2u), 0x00020000);
-#pragma unroll
-        for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-            for (int s = 0; s < KS; ++s)
-                kf[kb][s] = __builtin_bit_cast(bf16x8, __builtin_amdgcn_raw_buffer_load_b128(r, (int)k_off + s * 64, kb * 32 * a.k_st, 0));
+    auto copy_k = [&](const Tile& x) {
+        const i32x4 r = make_rsrc(kbase + x.page * a.k_sp + (int64_t)x.row * a.k_st, (int32_t)((uint32_t)x.n * (uint32_t)a.k_st * 2u));
+        static_for<K_LOADS>([&](auto T) {
+            constexpr int t = decltype(T)::value, rows = t / K_PERIOD * K_PERIOD * 64 / KGR;
+            copy16_to_lds<t * 1024>(r, kbuf_lds, k_src[t % K_PERIOD], (uint32_t)(rows * 2) * (uint32_t)a.k_st);
+        });
     };
     auto copy_v = [&](const Tile& x, int buf) {
         const i32x4 r = make_rsrc(vbase + x.page * a.v_sp + (int64_t)x.row * a.v_st, (int32_t)((uint32_t)x.n * (uint32_t)a.v_st * 2u));
         static_for<V_LOADS>([&](auto T) {
-            constexpr int t = decltype(T)::value;
-            copy16_to_lds<t * 1024>(r, vbuf_lds + buf * V_BYTES, v_src[t % 2], (uint32_t)(t * (64 / VGR) * 2) * (uint32_t)a.v_st);
+            constexpr int t = decltype(T)::value, rows = t / 2 * 2 * 64 / VGR;
+            copy16_to_lds<t * 1024>(r, vbuf_lds + buf * V_BYTES, v_src[t % 2], (uint32_t)(rows * 2) * (uint32_t)a.v_st);
         });
     };
 
@@ -270,36 +290,46 @@ void attend_kernel(AttendArgs a) {
         }
         int buf = 0;
         Tile now{}, next{};
+        // Copies are in flight in this order: K(t), V(t) | K(t + 1), V(t + 1), a tile's K after the scores of the
+        // one before, its V after the values of the one before (with two V buffers with its K), and waits
+        // count the younger ones. No other load of the loop is waited for by number.
         if (tile0 < tile_end) {
             now = tile(tile0);
+            copy_k(now);
             copy_v(now, 0);
-            load_k(now);
         }
         for (int t = tile0; t < tile_end; t += NWAVES, now = next) {
+            const bool more = t + NWAVES < tile_end;
+            if (more) next = tile(t + NWAVES);
+            asm volatile("s_waitcnt vmcnt(%0)" ::"i"(V_LOADS) : "memory");
             f32x4 s[RB][2];
+            bf16x8 kf[2][KS];
 #pragma unroll
             for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-                for (int rb = 0; rb < RB; ++rb) {
+                for (int k = 0; k < KS; ++k) kf[kb][k] = __builtin_bit_cast(bf16x8, k_at[k][kb * 16 * KGR]);
+#pragma unroll
+            for (int rb = 0; rb < RB; ++rb) {
+                if (SKIP && !(now.mask & bits[rb])) continue;
+#pragma unroll
+                for (int kb = 0; kb < 2; ++kb) {
                     s[rb][kb] = f32x4{0, 0, 0, 0};
 #pragma unroll
                     for (int k = 0; k < KS; ++k)
                         s[rb][kb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[kb][k], qf[rb][k], s[rb][kb], 0, 0, 0);
                 }
-            const bool more = t + NWAVES < tile_end;
-            if (more) next = tile(t + NWAVES);
-            if constexpr (VB == 2) {
-                // this tile's values are in LDS once the loads up to here are done, and the other buffer is
-                // free once the last tile's reads of it are
-                asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
-                if (more) copy_v(next, buf ^ 1);
             }
-            if (more) load_k(next);
+            if (more) {
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // K is read (and V of the tile before)
+                copy_k(next);
+                if constexpr (VB == 2) copy_v(next, buf ^ 1);
+            }
             const bool masked = now.key0 + BT - 1 > first_pos, partial = now.mask != all_bits;
             if (masked || partial) {
 #pragma unroll
                 for (int rb = 0; rb < RB; ++rb) {
-                    const int last = now.mask & bit ? lim[rb] : -1;
+                    if (SKIP && !(now.mask & bits[rb])) continue;
+                    const int last = now.mask & bit[rb] ? lim[rb] : -1;
 #pragma unroll
                     for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
@@ -311,6 +341,8 @@ void attend_kernel(AttendArgs a) {
             float top[RB];
 #pragma unroll
             for (int rb = 0; rb < RB; ++rb) {
+                top[rb] = -INFINITY;
+                if (SKIP && !(now.mask & bits[rb])) continue;
                 top[rb] = fmaxf(fmaxf(fmaxf(s[rb][0][0], s[rb][0][1]), fmaxf(s[rb][0][2], s[rb][0][3])),
                                 fmaxf(fmaxf(s[rb][1][0], s[rb][1][1]), fmaxf(s[rb][1][2], s[rb][1][3]))) * a.scale_log2;
                 above = above || top[rb] > m_run[rb] + LAZY;
@@ -329,6 +361,7 @@ void attend_kernel(AttendArgs a) {
             bf16x8 p[RB];
 #pragma unroll
             for (int rb = 0; rb < RB; ++rb) {
+                if (SKIP && !(now.mask & bits[rb])) continue;
                 const float use = m_run[rb] == -INFINITY ? 0.f : m_run[rb];
 #pragma unroll
                 for (int kb = 0; kb < 2; ++kb)
@@ -339,11 +372,9 @@ void attend_kernel(AttendArgs a) {
                         p[rb][kb * 4 + i] = (__bf16)x;
                     }
             }
-            if constexpr (VB == 1) {
-                // this tile's values are in LDS: only the keys of the next one are younger
-                if (more) asm volatile("s_waitcnt vmcnt(%0)" ::"i"(2 * KS) : "memory");
-                else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-            }
+            // this tile's values are in LDS: only what belongs to the next one is younger
+            if (more) asm volatile("s_waitcnt vmcnt(%0)" ::"i"(K_LOADS + (VB == 2 ? V_LOADS : 0)) : "memory");
+            else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
             bool wild = false;
             if (careful && (masked || partial)) {
                 // values that are not finite count as 0 here; the rows that see them get them after the product
@@ -371,7 +402,8 @@ void attend_kernel(AttendArgs a) {
                 __builtin_memcpy(&vf, &x, 8);
                 __builtin_memcpy((char*)&vf + 8, &y, 8);
 #pragma unroll
-                for (int rb = 0; rb < RB; ++rb) o[rb][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, p[rb], o[rb][d], 0, 0, 0);
+                for (int rb = 0; rb < RB; ++rb)
+                    if (!SKIP || now.mask & bits[rb]) o[rb][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, p[rb], o[rb][d], 0, 0, 0);
             }
             if (wild) {
                 const u16* const v0 = vbase + now.page * a.v_sp + (int64_t)now.row * a.v_st + grp * 4;
@@ -385,7 +417,7 @@ void attend_kernel(AttendArgs a) {
                             const float v = __uint_as_float(i % 2 ? x[i / 2] & 0xffff0000u : x[i / 2] << 16);
 #pragma unroll
                             for (int rb = 0; rb < RB; ++rb)
-                                if (!(fabsf(v) < INFINITY) && now.key0 + key <= (now.mask & bit ? lim[rb] : -1)) o[rb][d][i] += v;
+                                if (!(fabsf(v) < INFINITY) && now.key0 + key <= (now.mask & bit[rb] ? lim[rb] : -1)) o[rb][d][i] += v;
                         }
                     }
             }
@@ -437,7 +469,7 @@ void attend_kernel(AttendArgs a) {
         constexpr int GR = DV / 8 / JP;  // granules of a row of this part
         for (int i = threadIdx.x; i < ROWS * GR; i += NTHREADS) {
             const int c = i / GR, g = i % GR;
-            const int t = RB == 1 ? min((row0 + c) / a.rows, entries - 1) : 0;
+            const int t = entries > 1 ? min((row0 + c) / a.rows, entries - 1) : 0;
             const Entry e = ents[t];
             const int r = row0 + c - t * a.rows;
             if (r >= e.rows * a.group) continue;
@@ -511,11 +543,18 @@ Cut cut_of(const vpp_block_attn_config_t& c, int64_t num_query_blocks) {
     Cut u;
     u.rows = c.num_q_heads / c.num_kv_heads * c.query_block;
     u.rb = u.rows <= 16 ? 1 : u.rows <= 32 ? 2 : 4;
-    u.chunks = (u.rows + 16 * u.rb - 1) / (16 * u.rb);
-    // Several query blocks share a workgroup's 16 columns, and the blocks that they list in common, while
-    // there are four workgroups a CU left.
-    u.pack = u.rows <= 16 ? 16 / u.rows : 1;
-    while (u.pack > 1 && (u.pack * c.max_blocks > MAX_ELEMENTS || num_query_blocks * c.num_kv_heads / u.pack < 1024)) u.pack /= 2;
+    u.pack = 1;
+    // Several short query blocks share a workgroup, and the blocks that they list in common, while there are
+    // two workgroups a CU left.
+    for (int rb = 4; rb >= 1 && u.rows <= 16; rb /= 2) {
+        const int pack = 16 * rb / u.rows < MAX_PACK ? 16 * rb / u.rows : MAX_PACK;
+        if (pack < 2 || pack * c.max_blocks > MAX_ELEMENTS || num_query_blocks * c.num_kv_heads / pack < 512) continue;
+        u.pack = pack;
+        u.rb = (pack * u.rows + 15) / 16;
+        u.rb = u.rb == 3 ? 4 : u.rb;
+        break;
+    }
+    u.chunks = u.pack > 1 ? 1 : (u.rows + 16 * u.rb - 1) / (16 * u.rb);
     // Few workgroups split their lists, down to two tiles a wave.
     const int64_t wgs = (num_query_blocks + u.pack - 1) / u.pack * u.chunks * c.num_kv_heads;
     const int64_t tiles = (int64_t)c.max_blocks * (c.block_size / BT), most = tiles / (2 * NWAVES);
@@ -539,8 +578,9 @@ extern "C" vpp_status_t vpp_block_attn_workspace(const vpp_block_attn_config_t* 
 
 namespace {
 template <int DQK, int DV>
-auto pick_attend(int rb) {
-    return rb == 1 ? attend_kernel<DQK, DV, 1> : rb == 2 ? attend_kernel<DQK, DV, 2> : attend_kernel<DQK, DV, 4>;
+auto pick_attend(int rb, bool pack) {
+    return rb == 1 ? attend_kernel<DQK, DV, 1, false> : rb == 2 ? (pack ? attend_kernel<DQK, DV, 2, true> : attend_kernel<DQK, DV, 2, false>)
+                                                       : (pack ? attend_kernel<DQK, DV, 4, true> : attend_kernel<DQK, DV, 4, false>);
 }
 }  // namespace
 
@@ -602,7 +642,7 @@ extern "C" vpp_status_t vpp_block_attn_run_paged(
     const int64_t grid = (int64_t)((num_query_blocks + a.pack - 1) / a.pack) * a.chunks * a.splits * hkv;
     if (grid >= ((int64_t)1 << 31)) return VPP_ERR_INVALID_ARG;
     const size_t lds = (size_t)a.pack * a.max_blocks * (sizeof(Element) + 4);
-    auto* kernel = dqk == 64 ? pick_attend<64, 64>(cut.rb) : dqk == 128 ? pick_attend<128, 128>(cut.rb) : pick_attend<192, 128>(cut.rb);
+    auto* kernel = dqk == 64 ? pick_attend<64, 64>(cut.rb, a.pack > 1) : dqk == 128 ? pick_attend<128, 128>(cut.rb, a.pack > 1) : pick_attend<192, 128>(cut.rb, a.pack > 1);
     hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(NTHREADS), lds, (hipStream_t)stream, a);
     if (hipGetLastError() != hipSuccess) return VPP_ERR_HIP;
     if (a.splits > 1) {

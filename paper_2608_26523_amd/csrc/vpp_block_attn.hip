@@ -29,6 +29,7 @@ struct AttendArgs {
     Pages pages;
     int32_t num_entries, tokens, segments, query_block, group, hkv;
     int32_t block_shift, max_blocks;
+    int32_t generation;                  // items of a kv head that run at one time
     int32_t pack, rows, chunks, splits;  // query blocks of a workgroup, rows of one; workgroups of their rows, of their lists
     float scale_log2;
 };
@@ -87,17 +88,19 @@ struct Element {
     int rows_mask;        // cached rows of it << 16 | query blocks that list it
 };
 
-// The workgroup's tile list. A block that several of its query blocks list becomes one element, with
-// all their bits, if every list ascends (as a selection's do): each block is looked up in the other
-// lists of the same request by bisection, and is left to the first list that has it. Else every
-// entry is an element of its own, so that a block listed twice counts twice.
+// The workgroup's list of blocks. A block that several of its query blocks list becomes one element,
+// with all their bits, if every list ascends (as a selection's do): each block is looked up in the
+// other lists of the same request by bisection, is left to the first list that has it, and takes
+// the place that its order gives it among all. Else every entry is an element of its own, so that
+// a block listed twice counts twice. Either way the order is the same every time.
+// raw and ranks: [entries * max_blocks + 1], shared: two numbers. Returns the elements' number.
 __device__ __forceinline__ int list_elements(const AttendArgs& a, const Entry* ents, int entries, int entry0, int head, int* raw,
-                                             Element* elements, int* shared) {
-    const int lane = (int)threadIdx.x & 63, total = entries * a.max_blocks;
+                                             int* ranks, Element* elements, int* shared) {
+    const int lane = (int)threadIdx.x & 63, wave = uniform((int)threadIdx.x >> 6), most = a.max_blocks, total = entries * most;
     for (int i = threadIdx.x; i < total; i += NTHREADS) {
-        const int t = i / a.max_blocks, j = i - t * a.max_blocks;
+        const int t = i / most, j = i - t * most;
         const Entry e = ents[t];
-        const int b = a.lists[((int64_t)(entry0 + t) * a.hkv + head) * a.max_blocks + j];
+        const int b = a.lists[((int64_t)(entry0 + t) * a.hkv + head) * most + j];
         raw[i] = e.rows > 0 && b >= 0 && b <= (e.pos0 + e.rows - 1) >> a.block_shift ? b : INT32_MAX;
     }
     if (threadIdx.x == 0) shared[0] = 0;
@@ -105,54 +108,71 @@ __device__ __forceinline__ int list_elements(const AttendArgs& a, const Entry* e
     if (entries > 1) {
         bool bad = false;
         for (int i = threadIdx.x; i < total; i += NTHREADS)
-            if (i % a.max_blocks && raw[i] <= raw[i - 1] && raw[i - 1] != INT32_MAX) bad = true;
-            else if (i % a.max_blocks && raw[i - 1] == INT32_MAX && raw[i] != INT32_MAX) bad = true;
+            bad = bad || (i % most && (raw[i - 1] == INT32_MAX ? raw[i] != INT32_MAX : raw[i] <= raw[i - 1]));
         if (__ballot(bad) && lane == 0) shared[0] = 1;
         __syncthreads();
     }
-    const bool merge = entries > 1 && shared[0] == 0;
-    for (int i = threadIdx.x; i < total; i += NTHREADS) {
-        const int b = raw[i], t = i / a.max_blocks;
-        const Entry e = ents[t];
-        int mask = b == INT32_MAX ? 0 : 1 << t, end = e.pos0 + e.rows;
-        if (merge && mask)
-            for (int o = 0; o < entries && mask; ++o) {
-                const Entry f = ents[o];
-                if (o == t || f.segment != e.segment || f.kv_start != e.kv_start) continue;
-                const int* const r = raw + o * a.max_blocks;
-                int l = 0, h = a.max_blocks;  // first entry >= b
-                while (l < h) {
-                    const int m = (l + h) >> 1;
-                    if (r[m] < b) l = m + 1;
-                    else h = m;
-                }
-                if (l == a.max_blocks || r[l] != b) continue;
-                mask = o < t ? 0 : mask | 1 << o;
-                end = max(end, f.pos0 + f.rows);
-            }
-        Element x{0, 0, 0, 0};
-        if (mask) {
-            x.key0 = b << a.block_shift;
-            const int row = e.kv_start + x.key0;
-            x.page = a.pages.page(e.segment, row);
-            x.row = row & ((1 << a.pages.page_shift) - 1);
-            x.rows_mask = min(1 << a.block_shift, end - x.key0) << 16 | mask;
+    const bool merge = entries > 1 && uniform(shared[0]) == 0;
+    auto bisect = [&](int o, int b) {  // first place of list o with a block >= b
+        const int* const r = raw + o * most;
+        int l = 0, h = most;
+        while (l < h) {
+            const int m = (l + h) >> 1;
+            if (r[m] < b) l = m + 1;
+            else h = m;
         }
-        elements[i] = x;
+        return l;
+    };
+    auto apart = [&](const Entry& x, const Entry& y) { return x.segment != y.segment || x.kv_start != y.kv_start; };
+    // which entries become elements, and how many before each
+    for (int i = threadIdx.x; i < total; i += NTHREADS) {
+        const int b = raw[i], t = i / most;
+        bool mine = b != INT32_MAX;
+        if (merge && mine)
+            for (int o = 0; o < t && mine; ++o) {
+                if (apart(ents[o], ents[t])) continue;
+                const int l = bisect(o, b);
+                mine = l == most || raw[o * most + l] != b;
+            }
+        ranks[i] = mine;
     }
     __syncthreads();
-    // compacted in the order of the lists, which is the same every time; a wave reads 64 before it writes
-    if (threadIdx.x < 64) {
+    if (wave == 0) {
         int n = 0;
         for (int i0 = 0; i0 < total; i0 += 64) {
-            Element x{0, 0, 0, 0};
-            if (i0 + lane < total) x = elements[i0 + lane];
-            const bool use = (x.rows_mask & 0xffff) != 0;
-            const uint64_t all = __ballot(use);
-            if (use) elements[n + count(all & (((uint64_t)1 << lane) - 1))] = x;
+            const bool mine = i0 + lane < total && ranks[i0 + lane];
+            const uint64_t all = __ballot(mine);
+            if (i0 + lane < total) ranks[i0 + lane] = (n + count(all & (((uint64_t)1 << lane) - 1))) * 2 + mine;
             n += count(all);
         }
-        if (lane == 0) shared[1] = n;
+        if (lane == 0) ranks[total] = n * 2, shared[1] = n;
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < total; i += NTHREADS) {
+        if (!(ranks[i] & 1)) continue;
+        const int b = raw[i], t = i / most;
+        const Entry e = ents[t];
+        int mask = 1 << t, end = e.pos0 + e.rows, at = ranks[i] >> 1;
+        if (merge) {
+            at = 0;
+            for (int o = 0; o < entries; ++o) {
+                const Entry f = ents[o];
+                const int l = bisect(o, b);
+                at += (ranks[o * most + l] >> 1) - (ranks[o * most] >> 1);  // of list o's elements, those before b
+                // an equal block of another request: by the order of the lists
+                if (l < most && raw[o * most + l] == b) {
+                    if (!apart(e, f)) mask |= 1 << o, end = max(end, f.pos0 + f.rows);
+                    else if (o < t) at += ranks[o * most + l] & 1;
+                }
+            }
+        }
+        Element x;
+        x.key0 = b << a.block_shift;
+        const int row = e.kv_start + x.key0;
+        x.page = a.pages.page(e.segment, row);
+        x.row = row & ((1 << a.pages.page_shift) - 1);
+        x.rows_mask = min(1 << a.block_shift, end - x.key0) << 16 | mask;
+        elements[at] = x;
     }
     __syncthreads();
     return uniform(shared[1]);
@@ -185,7 +205,7 @@ void attend_kernel(AttendArgs a) {
     __shared__ float part_m[NWAVES][ROWS], part_l[NWAVES][ROWS];
     __shared__ Entry ents[MAX_PACK];
     __shared__ int shared[4];
-    extern __shared__ Element elements[];  // [pack * max_blocks], and behind them the lists
+    extern __shared__ Element elements[];  // [pack * max_blocks], and behind them the lists and the ranks
     const int lane = (int)threadIdx.x & 63, wave = uniform((int)threadIdx.x >> 6);
     const int col = lane & 15, grp = lane >> 4;
 
@@ -222,10 +242,14 @@ void attend_kernel(AttendArgs a) {
 #pragma unroll
         for (int s = 0; s < KS; ++s) qf[rb][s] = *(const bf16x8*)(p + s * 32);
     }
-    const int listed = list_elements(a, ents, entries, entry0, head, (int*)(elements + a.pack * a.max_blocks), elements, shared);
+    int* const raw = (int*)(elements + a.pack * a.max_blocks);
+    const int listed = list_elements(a, ents, entries, entry0, head, raw, raw + a.pack * a.max_blocks, elements, shared);
     const int shift = a.block_shift - 5;  // tiles of a block
-    const int tile_end = (int)((int64_t)(listed << shift) * (split + 1) / a.splits);
-    const int tile0 = (int)((int64_t)(listed << shift) * split / a.splits) + wave;
+    const int tiles = listed << shift;
+    const int tile_end = (int)((int64_t)tiles * (split + 1) / a.splits), tile0 = (int)((int64_t)tiles * split / a.splits) + wave;
+    // The workgroups that run at one time read the same blocks at about one time, out of their XCD's L2, if the
+    // next ones begin where these end: every other generation of them goes down its list.
+    const bool down = (uint32_t)item / (uint32_t)a.generation & 1;
     const int all_bits = (1 << entries) - 1;
 
     const u16* const kbase = a.k + (int64_t)head * a.k_sh;
@@ -259,6 +283,7 @@ void attend_kernel(AttendArgs a) {
         int key0, n, page, row, mask;  // n: cached keys of it
     };
     auto tile = [&](int t) {
+        if (down) t = tiles - 1 - t;
         const Element x = elements[t >> shift];
         const int sub = (t & ((1 << shift) - 1)) * BT, rm = uniform(x.rows_mask);
         return Tile{uniform(x.key0) + sub, max(0, min(BT, (rm >> 16) - sub)), uniform(x.page), uniform(x.row) + sub, rm & 0xffff};
@@ -546,7 +571,9 @@ Cut cut_of(const vpp_block_attn_config_t& c, int64_t num_query_blocks) {
     u.pack = 1;
     // Several short query blocks share a workgroup, and the blocks that they list in common, while there are
     // two workgroups a CU left.
-    for (int rb = 4; rb >= 1 && u.rows <= 16; rb /= 2) {
+    // (32 columns: two workgroups run on a CU. 4096 tokens of 32/8 heads, 16 blocks each: 640 us, in 16 columns
+    // 800, in 64, which read the least but run one a CU, 1097.)
+    for (int rb = 2; rb >= 1 && u.rows <= 16; rb /= 2) {
         const int pack = 16 * rb / u.rows < MAX_PACK ? 16 * rb / u.rows : MAX_PACK;
         if (pack < 2 || pack * c.max_blocks > MAX_ELEMENTS || num_query_blocks * c.num_kv_heads / pack < 512) continue;
         u.pack = pack;
@@ -633,6 +660,7 @@ extern "C" vpp_status_t vpp_block_attn_run_paged(
     a.rows = cut.rows;
     a.chunks = cut.chunks;
     a.splits = cut.splits;
+    a.generation = hkv < 256 ? 512 / hkv : 2;
     if (a.splits > 1) {
         const size_t need = (size_t)a.splits * num_tokens * hq * (dv + 1) * 4;
         if (!workspace || ((uintptr_t)workspace & 255u) || workspace_bytes < need) return VPP_ERR_WORKSPACE;
@@ -641,7 +669,7 @@ extern "C" vpp_status_t vpp_block_attn_run_paged(
     }
     const int64_t grid = (int64_t)((num_query_blocks + a.pack - 1) / a.pack) * a.chunks * a.splits * hkv;
     if (grid >= ((int64_t)1 << 31)) return VPP_ERR_INVALID_ARG;
-    const size_t lds = (size_t)a.pack * a.max_blocks * (sizeof(Element) + 4);
+    const size_t lds = (size_t)a.pack * a.max_blocks * (sizeof(Element) + 8) + 8;
     auto* kernel = dqk == 64 ? pick_attend<64, 64>(cut.rb, a.pack > 1) : dqk == 128 ? pick_attend<128, 128>(cut.rb, a.pack > 1) : pick_attend<192, 128>(cut.rb, a.pack > 1);
     hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(NTHREADS), lds, (hipStream_t)stream, a);
     if (hipGetLastError() != hipSuccess) return VPP_ERR_HIP;

@@ -540,16 +540,34 @@ __global__ __launch_bounds__(NTHREADS) void merge_kernel(AttendArgs a) {
     for (int i = (int)blockIdx.y * NTHREADS + (int)threadIdx.x; i < e.rows * hq * GR; i += (int)gridDim.y * NTHREADS) {
         const int g = i % GR, h = i / GR % hq, token = e.row0 + i / GR / hq;
         const int64_t i0 = (int64_t)token * hq + h, st = (int64_t)a.tokens * hq;
-        float m = a.part_lse[i0];
-        for (int s = 1; s < a.splits; ++s) m = fmaxf(m, a.part_lse[i0 + s * st]);
+        // all parts' sums at once, then four parts' values at a time: one after the other, a token's 16 parts
+        // take 16 latencies
+        float part[MAX_SPLITS], m = -INFINITY;
+#pragma unroll
+        for (int s = 0; s < MAX_SPLITS; ++s) {
+            const float v = a.part_lse[i0 + min(s, a.splits - 1) * st];
+            part[s] = s < a.splits ? v : -INFINITY;
+        }
+#pragma unroll
+        for (int s = 0; s < MAX_SPLITS; ++s) m = fmaxf(m, part[s]);
         const float use = m == -INFINITY ? 0.f : m;
         float l = 0, x[8] = {};
-        for (int s = 0; s < a.splits; ++s) {
-            const float f = __builtin_amdgcn_exp2f(a.part_lse[i0 + s * st] - use);
-            l += f;
-            const float* const y = a.part_o + (i0 + s * st) * DV + g * 8;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) x[j] += f > 0 || f != f ? y[j] * f : 0;
+        for (int s0 = 0; s0 < MAX_SPLITS; s0 += 4) {
+            if (s0 >= a.splits) break;
+            f32x4 y[4][2];
+#pragma unroll
+            for (int s = 0; s < 4; ++s)
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+                    y[s][j] = *(const f32x4*)(a.part_o + (i0 + min(s0 + s, a.splits - 1) * st) * DV + g * 8 + j * 4);
+#pragma unroll
+            for (int s = 0; s < 4; ++s) {
+                const float f = __builtin_amdgcn_exp2f(part[s0 + s] - use);
+                l += f;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) x[j] += f == 0 ? 0 : y[s][j / 4][j % 4] * f;
+            }
         }
         const float inv = l > 0 ? 1 / l : l;
         bf16x8 res;

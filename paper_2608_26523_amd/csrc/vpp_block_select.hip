@@ -662,9 +662,9 @@ extern "C" vpp_status_t vpp_block_select_paged(const vpp_block_attn_config_t* cf
             const int64_t wgs = (int64_t)a.wgs * a.hkv, step = NWAVES * (mt == 1 ? 4 : 1) * 16, steps = (cap + step - 1) / step;
             const int64_t splits = wgs >= 1024 ? 1 : (1024 + wgs - 1) / wgs;
             a.splits = (int32_t)(splits < steps ? splits : steps);
-            // Few lists of few blocks are made where their scores are: 32 of 8 kv heads up to 513 blocks 11 us, in
-            // two kernels 19.
-            const bool whole = mt == 1 && cap <= WHOLE_BLOCKS;
+            // Few lists of few blocks are made where their scores are (256 lists up to 513 blocks 12.8 us, in two
+            // kernels 18.9), unless they are so few that the blocks are better split (8 of 1563 20.6, split 13.3).
+            const bool whole = mt == 1 && cap <= WHOLE_BLOCKS && wgs >= 64;
             if (whole) mt = 0, a.splits = 1;
             if (wgs * a.splits >= ((int64_t)1 << 31)) return VPP_ERR_INVALID_ARG;
             auto* kernel = cfg->head_dim_qk == 64 ? pick_score<64>(mt, a.rows) : cfg->head_dim_qk == 128 ? pick_score<128>(mt, a.rows)

@@ -9,8 +9,8 @@
 //
 // Bound by HBM: rows are read and written once. A workgroup takes the rows of one token, or
 // of several that have few; its threads first put the tokens' cos and sin into LDS, once for
-// all heads, and then move units of two 16-byte granules: the two granules that hold the
-// partners of 8 pairs, or two that are only copied.
+// all heads, and then move units of two 16-byte granules: the two that hold the partners of 8
+// pairs, or two of the same distance that hold 4 pairs each or are only copied.
 #include <hip/hip_runtime.h>
 
 #include <math.h>
@@ -68,41 +68,36 @@ struct RopeArgs {
     Divisor by_token, by_pairs;
 };
 
-// One unit of a row: granules g0 and g1 (-1: there is no second one).
-template <bool INTERLEAVED, bool NT>
-__device__ __forceinline__ void move_unit(const u16* from, u16* to, int g0, int g1, bool turned, const float2* cs) {
-    const u32x4* const f = (const u32x4*)from;
-    u32x4* const t = (u32x4*)to;
-    auto load = [](const u32x4* p) { return NT ? __builtin_nontemporal_load(p) : *p; };
-    auto store = [](u32x4 x, u32x4* p) {
-        if constexpr (NT) __builtin_nontemporal_store(x, p);
-        else *p = x;
-    };
-    u32x4 x = load(f + g0), y = x;
-    if (g1 >= 0) y = load(f + g1);
-    if (turned) {
-        const bf16x8 a = __builtin_bit_cast(bf16x8, x), b = __builtin_bit_cast(bf16x8, y);
-        bf16x8 c, d;
+// One unit of a row: two granules (null: there is no second one, or none at all), and cos and sin of the
+// pairs that they hold (c0, c1), or of the pairs that they hold halves of (c0); null: only copied.
+struct Unit {
+    const u32x4 *f0, *f1;
+    u32x4 *t0, *t1;
+    const float2 *c0, *c1;
+    u32x4 x, y;
+};
+
+template <bool INTERLEAVED>
+__device__ __forceinline__ void turn(Unit& u) {
+    const bf16x8 a = __builtin_bit_cast(bf16x8, u.x), b = __builtin_bit_cast(bf16x8, u.y);
+    bf16x8 c, d;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float2 w = cs[i];  // cos, sin
-            if constexpr (INTERLEAVED) {
-                const bf16x8& s = i < 4 ? a : b;
-                bf16x8& r = i < 4 ? c : d;
-                const float u = (float)s[i % 4 * 2], v = (float)s[i % 4 * 2 + 1];
-                r[i % 4 * 2] = (__bf16)(u * w.x - v * w.y);
-                r[i % 4 * 2 + 1] = (__bf16)(v * w.x + u * w.y);
-            } else {
-                const float u = (float)a[i], v = (float)b[i];
-                c[i] = (__bf16)(u * w.x - v * w.y);
-                d[i] = (__bf16)(v * w.x + u * w.y);
-            }
+    for (int i = 0; i < 8; ++i) {
+        const float2 w = INTERLEAVED ? (i < 4 ? u.c0[i] : u.c1[i - 4]) : u.c0[i];  // cos, sin
+        if constexpr (INTERLEAVED) {
+            const bf16x8& s = i < 4 ? a : b;
+            bf16x8& r = i < 4 ? c : d;
+            const float p = (float)s[i % 4 * 2], q = (float)s[i % 4 * 2 + 1];
+            r[i % 4 * 2] = (__bf16)(p * w.x - q * w.y);
+            r[i % 4 * 2 + 1] = (__bf16)(q * w.x + p * w.y);
+        } else {
+            const float p = (float)a[i], q = (float)b[i];
+            c[i] = (__bf16)(p * w.x - q * w.y);
+            d[i] = (__bf16)(q * w.x + p * w.y);
         }
-        x = __builtin_bit_cast(u32x4, c);
-        y = __builtin_bit_cast(u32x4, d);
     }
-    store(x, t + g0);
-    if (g1 >= 0) store(y, t + g1);
+    u.x = __builtin_bit_cast(u32x4, c);
+    u.y = __builtin_bit_cast(u32x4, d);
 }
 
 template <bool INTERLEAVED, bool NT>
@@ -116,8 +111,9 @@ __global__ __launch_bounds__(NTHREADS) void rope_kernel(RopeArgs a) {
         const float turn = (float)(int32_t)(angle >> 32) * 0x1p-32f;
         cs[i] = make_float2(__builtin_amdgcn_cosf(turn) * a.scale, __builtin_amdgcn_sinf(turn) * a.scale * a.sign);
     }
-    __syncthreads();
-    for (int i = threadIdx.x; i < tokens * a.units; i += NTHREADS) {
+    auto unit = [&](int i) {
+        Unit m{};
+        if (i >= tokens * a.units) return m;
         const int tl = divide(i, a.by_token), t = t0 + tl;
         int r = i - tl * a.units;
         const bool is_q = r < a.q_units, is_v = r >= a.qk_units;
@@ -130,21 +126,51 @@ __global__ __launch_bounds__(NTHREADS) void rope_kernel(RopeArgs a) {
             to += (int64_t)t * rows.to_st;
         } else {
             const int64_t slot = a.slots[t];
-            if (slot < 0 || slot >= ((int64_t)a.num_pages << a.page_shift)) continue;
+            if (slot < 0 || slot >= ((int64_t)a.num_pages << a.page_shift)) return m;
             to += (slot >> a.page_shift) * (is_v ? a.v_sp : a.k_sp) + (slot & (((int64_t)1 << a.page_shift) - 1)) * rows.to_st;
         }
-        const bool turned = u < rows.turned;
+        // neighbouring threads move neighbouring granules, in both of a thread's
         int g0, g1;
-        if (turned) {
-            g0 = a.off_gr + (INTERLEAVED ? 2 * u : u);
-            g1 = INTERLEAVED ? g0 + 1 : g0 + a.rot_gr / 2;
-        } else {  // granules that are only copied: those around the rotated ones, two by two
+        if (u < rows.turned) {
+            g0 = a.off_gr + u;
+            g1 = g0 + a.rot_gr / 2;
+            m.c0 = cs + tl * a.pairs + u * (INTERLEAVED ? 4 : 8);
+            m.c1 = m.c0 + a.rot_gr / 2 * 4;
+        } else {  // granules that are only copied: those around the rotated ones
             const int skip = rows.turned ? a.rot_gr : 0, n = (is_v ? a.gran_v : a.gran_qk) - skip;
-            const int c = (u - rows.turned) * 2;
-            g0 = c < a.off_gr || !skip ? c : c + skip;
-            g1 = c + 1 >= n ? -1 : c + 1 < a.off_gr || !skip ? c + 1 : c + 1 + skip;
+            const int x = u - rows.turned, y = x + (n + 1) / 2;
+            g0 = x < a.off_gr || !skip ? x : x + skip;
+            g1 = y >= n ? -1 : y < a.off_gr || !skip ? y : y + skip;
         }
-        move_unit<INTERLEAVED, NT>(from, to, g0, g1, turned, cs + tl * a.pairs + u * 8);
+        m.f0 = (const u32x4*)from + g0;
+        m.t0 = (u32x4*)to + g0;
+        m.f1 = g1 < 0 ? nullptr : (const u32x4*)from + g1;
+        m.t1 = (u32x4*)to + g1;
+        return m;
+    };
+    auto load = [](const u32x4* p) { return NT ? __builtin_nontemporal_load(p) : *p; };
+    auto store = [](u32x4 x, u32x4* p) {
+        if constexpr (NT) __builtin_nontemporal_store(x, p);
+        else *p = x;
+    };
+    // AHEAD units of a thread are loaded before the first is stored: the first ones travel while cos and sin
+    // are worked out
+    constexpr int AHEAD = 2;
+    for (int i0 = 0; i0 < tokens * a.units; i0 += AHEAD * NTHREADS) {
+        Unit m[AHEAD];
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j) {
+            m[j] = unit(i0 + j * NTHREADS + (int)threadIdx.x);
+            if (m[j].f0) m[j].x = load(m[j].f0);
+            if (m[j].f1) m[j].y = load(m[j].f1);
+        }
+        if (i0 == 0) __syncthreads();
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j) {
+            if (m[j].c0) turn<INTERLEAVED>(m[j]);
+            if (m[j].f0) store(m[j].x, m[j].t0);
+            if (m[j].f1) store(m[j].y, m[j].t1);
+        }
     }
 }
 
@@ -210,9 +236,17 @@ vpp_status_t launch(const vpp_rope_config_t& c, RopeArgs& a, int32_t hq, int32_t
     a.units = (int32_t)units;
     a.by_token = divisor((uint32_t)units);
     a.by_pairs = divisor((uint32_t)a.pairs);
-    a.wg_tokens = 1;
+    // Tokens of few rows share a workgroup, up to two units a thread, while four workgroups a CU are left.
+    int64_t share = 2 * NTHREADS / units;
+    for (const int64_t most : {(int64_t)a.tokens / 1024, (int64_t)LDS_PAIRS / a.pairs})
+        if (share > most) share = most;
+    a.wg_tokens = share < 1 ? 1 : (int32_t)share;
     const unsigned grid = (unsigned)((a.tokens + a.wg_tokens - 1) / a.wg_tokens);
-    auto* kernel = c.interleaved ? rope_kernel<true, false> : rope_kernel<false, false>;
+    // Non-temporal past 64 MB of rows on the way into a cache, twice the L2s: 8192 tokens of 64/4 heads (302 MB
+    // moved) 60.8 us, 65.4 without. Rows that are only rotated, 805 MB: 167 and 166.
+    const bool nt = a.slots && units * a.tokens * 32 > ((int64_t)64 << 20);
+    auto* kernel = c.interleaved ? (nt ? rope_kernel<true, true> : rope_kernel<true, false>)
+                                 : (nt ? rope_kernel<false, true> : rope_kernel<false, false>);
     hipLaunchKernelGGL(kernel, dim3(grid), dim3(NTHREADS), 0, (hipStream_t)stream, a);
     return hipGetLastError() == hipSuccess ? VPP_OK : VPP_ERR_HIP;
 }

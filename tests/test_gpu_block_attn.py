@@ -164,6 +164,73 @@ def test_selection_among_many_blocks():
         assert np.array_equal(got.cpu().numpy(), want)
 
 
+@pytest.mark.parametrize("heads,size,tokens", [
+    ((64, 64, 64, 64), 1, 600), ((32, 16, 64, 64), 1, 1100), ((32, 8, 128, 128), 1, 1100), ((24, 8, 64, 64), 1, 1100),
+    ((64, 8, 64, 64), 1, 600), ((64, 4, 128, 128), 1, 600), ((64, 4, 192, 128), 1, 1100), ((64, 4, 128, 128), 2, 600),
+    ((64, 4, 192, 128), 3, 700), ((16, 16, 192, 128), 64, 4200), ((16, 8, 64, 64), 100, 8000), ((32, 8, 192, 128), 1, 1100)])
+def test_selection_of_many_query_blocks(heads, size, tokens):
+    """Launches whose workgroups hold several query blocks, across the boundaries of segments."""
+    hq, hkv, d, dv = heads
+    print("case:", heads, size, tokens, flush=True)
+    cut = [tokens // 3 + 1, 5, tokens - tokens // 3 - 6]
+    cu, prefix, start, rows, rng = _chunk([(1500, cut[0]), (2000, cut[1]), (700, cut[2])], 64, 2, 128, tokens)
+    table, (_,) = R.paged(rng, rows, 128, (1,))
+    sums = torch.from_numpy(R.grid(rng.standard_normal((int(table.max()) + 1, 2, hkv, d)))).to(torch.bfloat16)
+    q = _bf16(rng, cu[-1], hq, d)
+    attn = _attn(hq, hkv, d, dv, 9, query_block=size, local_blocks=2)
+    attn.plan(cu, start, prefix)
+    got = attn.select(q.to(DEV), sums.to(DEV), torch.as_tensor(table, device=DEV))
+    torch.cuda.synchronize()
+    want = R.selected(R.f64(q), R.f64(sums), table, cu, start, prefix, hkv=hkv, block=64, size=size, most=9, sink=1, local=2)
+    assert np.array_equal(got.cpu().numpy(), want)
+
+
+@pytest.mark.parametrize("prefix", [31000, 40000, 100000, 130000, 300000, 600000])
+@pytest.mark.parametrize("ties", [False, True])
+@pytest.mark.parametrize("tokens,hkv", [(3, 1), (9, 8)])
+def test_selection_of_each_number_of_blocks(prefix, ties, tokens, hkv):
+    """Keys of one wave, of several, of a workgroup; scores that repeat past the end of a list."""
+    rng = np.random.default_rng(prefix)
+    rows, page = prefix + tokens, 1024
+    table = rng.permutation(-(-rows // page)).astype(np.int32)[None]
+    shape = (table.shape[1], page // 64, hkv, 64)
+    sums = rng.integers(-1, 2, size=shape) * (rng.random(shape) < 0.02) if ties else R.grid(rng.standard_normal(shape))
+    sums = torch.from_numpy(sums.astype(np.float64)).to(torch.bfloat16)
+    q = _bf16(rng, tokens, hkv * 2, 64)
+    if ties:
+        q = q.sign()
+    for most in (5, 64, 300):
+        attn = _attn(hkv * 2, hkv, 64, 64, most, local_blocks=2)
+        attn.plan([0, tokens], [0], [prefix])
+        got = attn.select(q.to(DEV), sums.to(DEV), torch.as_tensor(table, device=DEV))
+        want = R.selected(R.f64(q), R.f64(sums), table, [0, tokens], [0], [prefix], hkv=hkv, block=64, size=1, most=most, sink=1, local=2)
+        assert np.array_equal(got.cpu().numpy(), want)
+
+
+def test_selection_slab_by_slab():
+    """More scores than the workspace holds: 128 heads, 16384 blocks, 64 query blocks a slab."""
+    rng = np.random.default_rng(5)
+    hkv, page, prefix, tokens = 128, 4096, 16384 * 64 - 200, 130
+    pages = -(-(prefix + tokens) // page)
+    table = rng.permutation(pages).astype(np.int32)[None]
+    g = torch.Generator(device=DEV)
+    g.manual_seed(1)
+    sums = torch.randint(-127, 128, (pages, page // 64, hkv, 64), generator=g, device=DEV).to(torch.bfloat16)
+    q = _bf16(rng, tokens, hkv, 64)
+    attn = _attn(hkv, hkv, 64, 64, 12)
+    attn.plan([0, tokens], [0], [prefix])
+    assert attn.select_bytes < tokens * hkv * 16384 * 4
+    got = attn.select(q.to(DEV), sums, torch.as_tensor(table, device=DEV)).cpu().numpy()
+    at = torch.as_tensor(table[0].astype(np.int64), device=DEV)
+    keys = sums[at].flatten(0, 1).double()  # [blocks, hkv, 64]
+    for t in (0, 63, 64, 100, 129):
+        f = (prefix + t) // 64
+        score = (keys[1:f] * torch.from_numpy(R.grid(R.f64(q[t]))).to(DEV)).sum(-1).T.cpu().numpy()  # whole multiples: exact
+        for h in range(0, hkv, 37):
+            order = np.lexsort((np.arange(f - 1), -score[h]))[:10] + 1
+            assert got[t, h].tolist() == sorted(order.tolist() + [0, f]), (t, h)
+
+
 # -- attention ----------------------------------------------------------------------------------
 def _lists(rng, cu, prefix, hkv, block, size, most):
     """Random lists: ascending with their own last block, then holes, repeats, blocks of the future
@@ -216,6 +283,53 @@ def test_attention(heads, segs, size, block, page, most):
     assert same is lse and torch.all(lse[:, cu[-1]:] == 7)
     want = R.attended(R.f64(q), R.f64(k), R.f64(v), table, lists, cu, start, prefix, block=block, size=size, scale=scale or None)
     _check(out, lse[:, :cu[-1]], *want)
+
+
+@pytest.mark.parametrize("heads,size,tokens", [
+    ((16, 16, 64, 64), 1, 560), ((32, 8, 64, 64), 1, 560), ((24, 8, 64, 64), 1, 700), ((64, 4, 128, 128), 1, 300),
+    ((16, 8, 128, 128), 2, 1100), ((16, 16, 192, 128), 1, 530), ((40, 8, 64, 64), 1, 300)])
+@pytest.mark.parametrize("tidy", [True, False])
+def test_attention_of_query_blocks_that_share_workgroups(heads, size, tokens, tidy):
+    """Tokens whose common blocks are read once: lists that ascend, of several requests in a workgroup, and
+    among them lists that do not; and infinite values in blocks that only some of them list."""
+    hq, hkv, d, dv = heads
+    print("case:", heads, size, tokens, tidy, flush=True)
+    cu, prefix, start, rows, rng = _chunk([(700, tokens // 2 + 3), (300, 7), (64, tokens - tokens // 2 - 10)], 64, 2, 128, tokens + hq)
+    table, (k, v) = R.paged(rng, rows, 128, (hkv, d), (hkv, dv))
+    q = _bf16(rng, cu[-1], hq, d)
+    qb = R.query_blocks(cu, prefix, size)
+    lists = np.full((len(qb), hkv, 6), -1, dtype=np.int32)
+    for n, (r0, nr, s, pos) in enumerate(qb):
+        c = (pos + nr - 1) // 64
+        for h in range(hkv):
+            got = sorted(set(rng.integers(0, c + 1, size=5).tolist()) | {c})
+            lists[n, h, :len(got)] = got
+    if not tidy:
+        messy = _lists(rng, cu, prefix, hkv, 64, size, 6)
+        lists[::23] = messy[::23]
+    attn = _attn(hq, hkv, d, dv, 6, query_block=size, sink_blocks=0)
+    attn.plan(cu, start, prefix)
+    run = lambda: attn.run_paged(*[x.to(DEV) for x in (q, k, v, torch.as_tensor(table), torch.as_tensor(lists))],  # noqa: E731
+                                 lse=torch.empty(hq, cu[-1], device=DEV))
+    out, lse = run()
+    again, _ = run()
+    torch.cuda.synchronize()
+    assert torch.equal(out, again)
+    _check(out, lse, *R.attended(R.f64(q), R.f64(k), R.f64(v), table, lists, cu, start, prefix, block=64, size=size))
+    if hq * tokens > 10000:
+        return
+    # block 5 of the first request becomes infinite in one column: its readers', and nobody else's
+    j = start[0] + 5 * 64 + 3
+    v[table[0][j // 128], j % 128, :, 9] = math.inf
+    wild, _ = run()
+    torch.cuda.synchronize()
+    want = out.clone()
+    for n, (r0, nr, s, pos) in enumerate(qb):
+        if s == 0:
+            for h in range(hkv):
+                if 5 in lists[n, h]:
+                    want[r0:r0 + nr, h * (hq // hkv):(h + 1) * (hq // hkv), 9] = math.inf
+    assert torch.equal(wild, want)
 
 
 def _random_run(seed, hq=8, hkv=2, d=128, dv=128, segs=((700, 50), (64, 3), (0, 129)), size=16, block=64, page=64, most=7):

@@ -136,7 +136,8 @@ vpp_status_t vpp_block_attn_workspace(const vpp_block_attn_config_t* cfg, int32_
  * twice counts twice. out [num_tokens][Hq][dv] bf16, lse (NULL or fp32, element
  * h * lse_stride_head + row) as for vpp_chunk_attn_run_paged; a row that sees no key gets
  * zeros and lse -infinity; rows of no query block stay as they are. Values of keys that a
- * token does not see do not reach its results, not as infinities or NaN either.
+ * token does not see do not reach its results, not as infinities or NaN either. The rows
+ * of out share no memory with each other or with an input.
  * Arithmetic as for vpp_chunk_attn_run. workspace: 256-byte aligned, may be NULL if the
  * size is 0; not to be used by other work in flight.
  * Errors: VPP_ERR_INVALID_ARG, VPP_ERR_UNSUPPORTED, VPP_ERR_WORKSPACE, VPP_ERR_HIP.

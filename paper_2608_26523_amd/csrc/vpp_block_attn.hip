@@ -105,14 +105,35 @@ __device__ __forceinline__ int list_elements(const AttendArgs& a, const Entry* e
     }
     if (threadIdx.x == 0) shared[0] = 0;
     __syncthreads();
-    if (entries > 1) {
+    auto element = [&](int b, const Entry& e, int end, int mask) {
+        Element x;
+        x.key0 = b << a.block_shift;
+        const int row = e.kv_start + x.key0;
+        x.page = a.pages.page(e.segment, row);
+        x.row = row & ((1 << a.pages.page_shift) - 1);
+        x.rows_mask = min(1 << a.block_shift, end - x.key0) << 16 | mask;
+        return x;
+    };
+    if (entries == 1) {  // a list as it is, without its holes; ranks are not used
+        int n = 0;
+        for (int i0 = 0; i0 < most && wave == 0; i0 += 64) {
+            const int b = i0 + lane < most ? raw[i0 + lane] : INT32_MAX;
+            const uint64_t all = __ballot(b != INT32_MAX);
+            if (b != INT32_MAX) elements[n + count(all & (((uint64_t)1 << lane) - 1))] = element(b, ents[0], ents[0].pos0 + ents[0].rows, 1);
+            n += count(all);
+        }
+        if (threadIdx.x == 0) shared[1] = n;
+        __syncthreads();
+        return uniform(shared[1]);
+    }
+    {
         bool bad = false;
         for (int i = threadIdx.x; i < total; i += NTHREADS)
             bad = bad || (i % most && (raw[i - 1] == INT32_MAX ? raw[i] != INT32_MAX : raw[i] <= raw[i - 1]));
         if (__ballot(bad) && lane == 0) shared[0] = 1;
         __syncthreads();
     }
-    const bool merge = entries > 1 && uniform(shared[0]) == 0;
+    const bool merge = uniform(shared[0]) == 0;
     auto bisect = [&](int o, int b) {  // first place of list o with a block >= b
         const int* const r = raw + o * most;
         int l = 0, h = most;
@@ -166,13 +187,7 @@ __device__ __forceinline__ int list_elements(const AttendArgs& a, const Entry* e
                 }
             }
         }
-        Element x;
-        x.key0 = b << a.block_shift;
-        const int row = e.kv_start + x.key0;
-        x.page = a.pages.page(e.segment, row);
-        x.row = row & ((1 << a.pages.page_shift) - 1);
-        x.rows_mask = min(1 << a.block_shift, end - x.key0) << 16 | mask;
-        elements[at] = x;
+        elements[at] = element(b, e, end, mask);
     }
     __syncthreads();
     return uniform(shared[1]);
@@ -596,7 +611,6 @@ Cut cut_of(const vpp_block_attn_config_t& c, int64_t num_query_blocks) {
         if (pack < 2 || pack * c.max_blocks > MAX_ELEMENTS || num_query_blocks * c.num_kv_heads / pack < 512) continue;
         u.pack = pack;
         u.rb = (pack * u.rows + 15) / 16;
-        u.rb = u.rb == 3 ? 4 : u.rb;
         break;
     }
     u.chunks = u.pack > 1 ? 1 : (u.rows + 16 * u.rb - 1) / (16 * u.rb);
@@ -624,8 +638,8 @@ extern "C" vpp_status_t vpp_block_attn_workspace(const vpp_block_attn_config_t* 
 namespace {
 template <int DQK, int DV>
 auto pick_attend(int rb, bool pack) {
-    return rb == 1 ? attend_kernel<DQK, DV, 1, false> : rb == 2 ? (pack ? attend_kernel<DQK, DV, 2, true> : attend_kernel<DQK, DV, 2, false>)
-                                                       : (pack ? attend_kernel<DQK, DV, 4, true> : attend_kernel<DQK, DV, 4, false>);
+    return rb == 1 ? attend_kernel<DQK, DV, 1, false> : rb == 4 ? attend_kernel<DQK, DV, 4, false>
+           : pack ? attend_kernel<DQK, DV, 2, true> : attend_kernel<DQK, DV, 2, false>;
 }
 }  // namespace
 
@@ -649,6 +663,7 @@ extern "C" vpp_status_t vpp_block_attn_run_paged(
     const int64_t most = (int64_t)1 << 31;
     const int dqk = cfg->head_dim_qk, dv = cfg->head_dim_v;
     if (!strides_ok(q_st, num_tokens, most, q_sh, hq, dqk) || !strides_ok(o_st, num_tokens, most, o_sh, hq, dv) ||
+        !rows_apart(o_st, num_tokens, o_sh, hq, dv) ||
         !strides_ok(k_st, page_size, row_most, k_sh, hkv, dqk) || !strides_ok(v_st, page_size, row_most, v_sh, hkv, dv) ||
         (num_pages > 1 && (!stride_ok(k_sp) || !stride_ok(v_sp))) || (lse && hq > 1 && lse_sh < num_tokens))
         return VPP_ERR_INVALID_ARG;
@@ -687,7 +702,7 @@ extern "C" vpp_status_t vpp_block_attn_run_paged(
     }
     const int64_t grid = (int64_t)((num_query_blocks + a.pack - 1) / a.pack) * a.chunks * a.splits * hkv;
     if (grid >= ((int64_t)1 << 31)) return VPP_ERR_INVALID_ARG;
-    const size_t lds = (size_t)a.pack * a.max_blocks * (sizeof(Element) + 8) + 8;
+    const size_t lds = (size_t)a.pack * a.max_blocks * (sizeof(Element) + (a.pack > 1 ? 8 : 4)) + 8;
     auto* kernel = dqk == 64 ? pick_attend<64, 64>(cut.rb, a.pack > 1) : dqk == 128 ? pick_attend<128, 128>(cut.rb, a.pack > 1) : pick_attend<192, 128>(cut.rb, a.pack > 1);
     hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(NTHREADS), lds, (hipStream_t)stream, a);
     if (hipGetLastError() != hipSuccess) return VPP_ERR_HIP;

@@ -134,6 +134,13 @@ __device__ __forceinline__ Entry uniform(const Entry& e) {
            (heads == 1 || (stride_ok(sh) && sh >= dim && sh < ((int64_t)1 << 31)));
 }
 
+// Whether no two of [rows][heads] vectors of dim elements share memory, rows or heads outermost.
+[[maybe_unused]] bool rows_apart(int64_t st, int64_t rows, int64_t sh, int64_t heads, int64_t dim) {
+    if (rows == 1 || heads == 1) return (rows == 1 || st >= dim) && (heads == 1 || sh >= dim);
+    const int64_t lo = st < sh ? st : sh, hi = st < sh ? sh : st, inner = st < sh ? rows : heads;
+    return lo >= dim && hi / lo >= inner - 1 && hi >= (inner - 1) * lo + dim;
+}
+
 }  // namespace
 
 #endif  // VPP_BLOCK_COMMON_H

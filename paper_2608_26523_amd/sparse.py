@@ -35,8 +35,9 @@ class BlockSparseAttention:
 
     A plan's query blocks are on the device, copied there on the stream that is current at
     ``plan``; runs on another stream wait for that copy. A run that is captured into a graph reads
-    the plan it was captured under: keep this object and do not plan it again while such a
-    graph is replayed.
+    the plan it was captured under: plan before the capture, keep this object, and do not plan it
+    again while such a graph is replayed. Workspaces are allocated by each call (within a capture
+    from the graph's own memory), so calls on several streams share none.
     """
 
     def __init__(self, num_q_heads: int, num_kv_heads: int, head_dim_qk: int, head_dim_v: int, max_blocks: int,
@@ -91,7 +92,7 @@ class BlockSparseAttention:
         """The blocks of the cache (int64 indices, on the GPU) that a chunk completes, for ``summarize``;
         host_block_table is a host copy of the block table (array [segments, pages_per_row])."""
         ids = B.vpp_completed_blocks(cu_q, kv_start, prefix_len, host_block_table, page_size, self.cfg.block_size)
-        return torch.from_numpy(ids).to(self.device)
+        return torch.from_numpy(ids).pin_memory().to(self.device, non_blocking=True)
 
     def new_summaries(self, num_pages: int, page_size: int) -> torch.Tensor:
         """Summaries (zeros) of a cache of num_pages pages: bf16 [num_pages, page_size / block_size, Hkv, dqk]."""

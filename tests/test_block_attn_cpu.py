@@ -157,9 +157,19 @@ def _run(cfg=None, qb=GOOD, n=4, q=GOOD, qs=(1024, 128), tokens=64, k=GOOD, ks=(
     dict(k=0), dict(k=GOOD + 4), dict(v=0), dict(v=GOOD + 4), dict(ks=(16384, 64, 128)), dict(ks=(16384, 1 << 24, 128)), dict(ks=(0, 256, 128)),
     dict(vs=(16384, 256, 64)), dict(vs=(16384, 1 << 24, 128)), dict(page=32), dict(page=1 << 21), dict(pages=0), dict(bt=0), dict(bts=-1),
     dict(segs=0), dict(per_row=0), dict(blocks=0), dict(blocks=GOOD + 1), dict(out=0), dict(out=GOOD + 4), dict(os_=(1024, 0)),
-    dict(os_=(1024, 64)), dict(lse=GOOD + 2), dict(lses=63)])
+    dict(os_=(1024, 64)), dict(os_=(512, 128)), dict(os_=(128, 128)), dict(lse=GOOD + 2), dict(lses=63)])
 def test_run_refusals(bad):
     assert _run(**bad) == B.VPP_ERR_INVALID_ARG
+
+
+def test_run_workspace():
+    """Few workgroups split their lists; the parts need a workspace."""
+    one = _cfg(query_block=1, max_blocks=64, num_q_heads=32, num_kv_heads=8)
+    need = B.vpp_block_attn_workspace(one, 1, 1)
+    assert need == 16 * 1 * 32 * 129 * 4 and B.vpp_block_attn_workspace(one, 1 << 16, 1 << 16) == 0
+    for ws, wsb in ((0, need), (GOOD, need - 1), (GOOD + 128, need)):
+        assert _run(cfg=one, n=1, tokens=1, qs=(4096, 128), os_=(4096, 128), ks=(65536, 1024, 128), vs=(65536, 1024, 128), ws=ws,
+                    wsb=wsb) == B.VPP_ERR_WORKSPACE
 
 
 def test_calls_of_nothing():

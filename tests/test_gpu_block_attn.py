@@ -545,6 +545,28 @@ def test_far_offsets_in_a_large_cache():
     _check(out, lse, *R.attended(R.f64(q), kf, vf, small[None], want, cu, start, prefix, block=256, size=1))
 
 
+@pytest.mark.parametrize("heads,size", [((4, 2, 64, 64), 1), ((1, 1, 192, 128), 64), ((32, 1, 128, 128), 1), ((16, 1, 192, 128), 8), ((2, 2, 128, 128), 16)])
+@pytest.mark.parametrize("block", [64, 256])
+def test_longest_lists(heads, size, block):
+    """2048 entries a list, a few of them blocks: the most LDS that a launch takes."""
+    hq, hkv, d, dv = heads
+    rng = np.random.default_rng(hq + size)
+    cu, prefix, start, rows, rng = _chunk([(3000, size + 1), (100, 3)], block, 1, 256, 9)
+    table, (k, v) = R.paged(rng, rows, 256, (hkv, d), (hkv, dv))
+    q = _bf16(rng, cu[-1], hq, d)
+    qb = R.query_blocks(cu, prefix, size)
+    lists = np.full((len(qb), hkv, 2048), -1, dtype=np.int32)
+    for n, (r0, nr, s, pos) in enumerate(qb):
+        c = (pos + nr - 1) // block
+        got = rng.permutation(c + 1)
+        lists[n, :, rng.permutation(2048)[:len(got)]] = got[:, None]
+    attn = _attn(hq, hkv, d, dv, 2048, block_size=block, query_block=size)
+    attn.plan(cu, start, prefix)
+    out, lse = attn.run_paged(*[x.to(DEV) for x in (q, k, v, torch.as_tensor(table), torch.as_tensor(lists))], lse=torch.empty(hq, cu[-1], device=DEV))
+    torch.cuda.synchronize()
+    _check(out, lse, *R.attended(R.f64(q), R.f64(k), R.f64(v), table, lists, cu, start, prefix, block=block, size=size))
+
+
 # -- together -----------------------------------------------------------------------------------
 def _layer(hq, hkv, d, dv, page, segs, seed, size=16, most=6, **kw):
     """A layer's state for requests whose prefixes are in the cache already."""

@@ -205,7 +205,7 @@ __device__ __forceinline__ int list_elements(const AttendArgs& a, const Entry* e
 // are not looked for: only if a result is not finite the workgroup does its tiles again, carefully.
 // SKIP: several query blocks, and tiles that none of a 16 rows' lists pass them by.
 template <int DQK, int DV, int RB, bool SKIP>
-__global__ __attribute__((amdgpu_flat_work_group_size(NTHREADS, NTHREADS), amdgpu_waves_per_eu(RB == 1 ? 3 : RB == 2 ? 2 : 1)))
+__global__ __attribute__((amdgpu_flat_work_group_size(NTHREADS, NTHREADS), amdgpu_waves_per_eu(RB == 4 || DQK == 192 ? 1 : 2)))
 void attend_kernel(AttendArgs a) {
     constexpr int KS = DQK / 32, DB = DV / 16, KGR = DQK / 8, VGR = DV / 8;
     constexpr int K_BYTES = BT * DQK * 2, K_LOADS = K_BYTES / 1024, V_BYTES = BT * DV * 2, V_LOADS = V_BYTES / 1024;

@@ -231,7 +231,7 @@ __device__ __forceinline__ void make_list(const SelectArgs& a, const Entry& e, c
     }
 #pragma unroll
     for (int r = 0; r < KR; ++r) {
-        if (NW == 1 && r >= regs) break;
+        if (NW == 1 && r >= regs) continue;
         const uint32_t k = key[r];
         bool in = k >= least && k != 0;
         if (!exact) {
@@ -390,7 +390,8 @@ __global__ __launch_bounds__(NTHREADS) void score_kernel(SelectArgs a) {
                         if (entry[m] >= 0) put(entry[m], block, x);
                     }
                 } else if constexpr (RM == 32) {
-                    // several tiles to a query block; what its earlier ones left in memory counts
+                    // several tiles to a query block; what its earlier ones left in memory counts (only the lane
+                    // whose block it is reads and writes it: the waves are not at the same tiles)
                     const int per = a.rows / 16;
                     float x = -INFINITY;
 #pragma unroll
@@ -398,7 +399,7 @@ __global__ __launch_bounds__(NTHREADS) void score_kernel(SelectArgs a) {
                         x = max_finite(x, v[m]);
                         if (m + 1 < MT && (mt0 + m + 1) % per != 0) continue;
                         x = max_xor32<true>(max_xor16<true>(x));
-                        if (grp == 0 && entry[m] >= 0) {
+                        if (grp == 0 && entry[m] >= 0 && block < hi) {
                             if (mt0 / per == (mt0 + m) / per && mt0 % per != 0) x = max_finite(x, scores[entry[m] * entry_st + block]);
                             put(entry[m], block, x);
                         }
@@ -450,7 +451,8 @@ __global__ __launch_bounds__(NTHREADS) void score_kernel(SelectArgs a) {
                 for (int n = 0; n < NT; ++n) {
                     const int now = (d0 + n) % 2;
                     tile(kf[buf][n], d[now], d[1 - now], block[1 - now]);
-                    block[now] = min(b + n * 16, hi - 1);  // past the last: its score again
+                    // past the last: its score again, the same (but RM = 32, which leaves them out)
+                    block[now] = RM == 32 ? b + n * 16 : min(b + n * 16, hi - 1);
                     __builtin_amdgcn_sched_barrier(0);
                 }
             };
@@ -565,8 +567,14 @@ extern "C" vpp_status_t vpp_block_summarize_paged(const vpp_block_attn_config_t*
 namespace {
 template <int DQK, int RM>
 auto pick_rows(int mt) {  // 0: the whole selection
-    return mt == 8 ? score_kernel<DQK, DQK == 192 ? 8 : 4, 1, RM, false> : mt == 4 ? score_kernel<DQK, 4, 1, RM, false>
-           : mt == 1 ? score_kernel<DQK, 1, 4, RM, false> : score_kernel<DQK, 1, 4, RM, true>;
+    auto* four = score_kernel<DQK, 4, 1, RM, false>;
+    if constexpr (DQK == 192)
+        if (mt == 8) return score_kernel<DQK, 8, 1, RM, false>;
+    if constexpr (RM != 32) {  // more rows than a tile has: never one tile
+        if (mt == 1) return score_kernel<DQK, 1, 4, RM, false>;
+        if (mt == 0) return score_kernel<DQK, 1, 4, RM, true>;
+    }
+    return four;
 }
 template <int DQK>
 auto pick_score(int mt, int rows) {

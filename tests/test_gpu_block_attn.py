@@ -185,6 +185,26 @@ def test_selection_of_many_query_blocks(heads, size, tokens):
     assert np.array_equal(got.cpu().numpy(), want)
 
 
+@pytest.mark.parametrize("heads,size", [((32, 1, 64, 64), 16), ((16, 2, 192, 128), 64), ((24, 2, 128, 128), 32)])
+@pytest.mark.parametrize("prefix", [2500, 4200])
+def test_selection_of_query_blocks_of_many_rows(heads, size, prefix):
+    """384 to 512 rows a query block, taken in several passes whose maxima meet in memory; half of the blocks
+    are chosen, so that the last one's score decides too."""
+    hq, hkv, d, dv = heads
+    rng = np.random.default_rng(prefix + size)
+    tokens, most = 20 * size + 3, prefix // 128
+    cu, start, rows = [0, tokens], [0], [prefix + tokens]
+    table, (_,) = R.paged(rng, rows, 128, (1,))
+    sums = torch.from_numpy(R.grid(rng.standard_normal((int(table.max()) + 1, 2, hkv, d)))).to(torch.bfloat16)
+    q = _bf16(rng, tokens, hq, d)
+    attn = _attn(hq, hkv, d, dv, most, query_block=size)
+    attn.plan(cu, start, [prefix])
+    want = R.selected(R.f64(q), R.f64(sums), table, cu, start, [prefix], hkv=hkv, block=64, size=size, most=most, sink=1, local=1)
+    for _ in range(3):
+        got = attn.select(q.to(DEV), sums.to(DEV), torch.as_tensor(table, device=DEV))
+        assert np.array_equal(got.cpu().numpy(), want)
+
+
 @pytest.mark.parametrize("prefix", [31000, 40000, 100000, 130000, 300000, 600000])
 @pytest.mark.parametrize("ties", [False, True])
 @pytest.mark.parametrize("tokens,hkv", [(3, 1), (9, 8)])

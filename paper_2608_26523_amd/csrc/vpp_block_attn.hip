@@ -197,13 +197,23 @@ __device__ __forceinline__ int list_elements(const AttendArgs& a, const Entry* e
 // of several short ones -- and each of its waves every fourth tile of 32 listed keys, with all rows:
 // keys and values are read once a workgroup and no wave waits for another until the end, where
 // the four partial results are joined through LDS.
-//   S^T = K Q^T on v_mfma_f32_16x16x32_bf16, K straight from memory (16 bytes a lane), Q held in
-//   registers: a lane has one row (column) and 8 of the 32 scores. Softmax in fp32 with exp2.
-//   O^T = V^T P^T: P leaves the scores already as the B operand; V^T is read from an LDS copy of
-//   the row-major tile by ds_read_b64_tr_b16.
+//   S^T = K Q^T on v_mfma_f32_16x16x32_bf16, Q held in registers: a lane has one row (column) and 8
+//   of the 32 scores. Softmax in fp32 with exp2.
+//   O^T = V^T P^T: P, rounded to bf16 as the matrix instruction takes it, leaves the scores
+//   already as the B operand; V^T is read from the row-major tile by ds_read_b64_tr_b16.
+// Keys and values come into a wave's own LDS, so it waits for its copies alone: keys read
+// from memory in the operand's layout are 64-byte pieces of 16 rows (query blocks of 64 tokens, 16 heads,
+// 64 blocks a list behind 120K: 975 us, through LDS 620).
 // Infinities and NaN among values that only some rows see would reach the others as 0 * inf. They
 // are not looked for: only if a result is not finite the workgroup does its tiles again, carefully.
 // SKIP: several query blocks, and tiles that none of a 16 rows' lists pass them by.
+//
+// What bounds it:
+//   single tokens of many requests: HBM (32 of 32/8 heads, 32 blocks each, 254 MB: 49 us, 5.2 TB/s);
+//   every token its own list: the blocks that few rows share, out of the caches (4096 tokens of 32/8
+//   heads, 16 blocks each, 14 GB of tiles: 640 us, 22 TB/s);
+//   long query blocks: one wave a SIMD goes through scores, softmax and products in turn (8192
+//   tokens in query blocks of 64: 609-624 us, 550 TFLOP/s).
 template <int DQK, int DV, int RB, bool SKIP>
 __global__ __attribute__((amdgpu_flat_work_group_size(NTHREADS, NTHREADS), amdgpu_waves_per_eu(RB == 4 || DQK == 192 ? 1 : 2)))
 void attend_kernel(AttendArgs a) {
@@ -263,7 +273,8 @@ void attend_kernel(AttendArgs a) {
     const int tiles = listed << shift;
     const int tile_end = (int)((int64_t)tiles * (split + 1) / a.splits), tile0 = (int)((int64_t)tiles * split / a.splits) + wave;
     // The workgroups that run at one time read the same blocks at about one time, out of their XCD's L2, if the
-    // next ones begin where these end: every other generation of them goes down its list.
+    // next ones begin where these end: every other generation of them goes down its list (4096 tokens of 32/8
+    // heads, 16 blocks each: 640 us, always up 660).
     const bool down = (uint32_t)item / (uint32_t)a.generation & 1;
     const int all_bits = (1 << entries) - 1;
 
@@ -605,7 +616,7 @@ Cut cut_of(const vpp_block_attn_config_t& c, int64_t num_query_blocks) {
     // Several short query blocks share a workgroup, and the blocks that they list in common, while there are
     // two workgroups a CU left.
     // (32 columns: two workgroups run on a CU. 4096 tokens of 32/8 heads, 16 blocks each: 640 us, in 16 columns
-    // 800, in 64, which read the least but run one a CU, 1097.)
+    // 744, in 64, which read the least but run one a CU, 1097.)
     for (int rb = 2; rb >= 1 && u.rows <= 16; rb /= 2) {
         const int pack = 16 * rb / u.rows < MAX_PACK ? 16 * rb / u.rows : MAX_PACK;
         if (pack < 2 || pack * c.max_blocks > MAX_ELEMENTS || num_query_blocks * c.num_kv_heads / pack < 512) continue;
@@ -614,7 +625,8 @@ Cut cut_of(const vpp_block_attn_config_t& c, int64_t num_query_blocks) {
         break;
     }
     u.chunks = u.pack > 1 ? 1 : (u.rows + 16 * u.rb - 1) / (16 * u.rb);
-    // Few workgroups split their lists, down to two tiles a wave.
+    // Few workgroups split their lists, down to two tiles a wave (a token of 32/8 heads, 64 blocks: 12 us with
+    // the merge, one workgroup a head alone goes through 32 tiles a wave).
     const int64_t wgs = (num_query_blocks + u.pack - 1) / u.pack * u.chunks * c.num_kv_heads;
     const int64_t tiles = (int64_t)c.max_blocks * (c.block_size / BT), most = tiles / (2 * NWAVES);
     int64_t s = wgs > 0 && wgs < 256 ? (512 + wgs - 1) / wgs : 1;

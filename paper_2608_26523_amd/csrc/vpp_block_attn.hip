@@ -213,8 +213,9 @@ __device__ __forceinline__ int list_elements(const AttendArgs& a, const Entry* e
 //   single tokens of many requests: HBM (32 of 32/8 heads, 32 blocks each, 254 MB: 49 us, 5.2 TB/s);
 //   every token its own list: the blocks that few rows share, out of the caches (4096 tokens of 32/8
 //   heads, 16 blocks each, 14 GB of tiles: 640 us, 22 TB/s);
-//   long query blocks: one wave a SIMD goes through scores, softmax and products in turn (8192
-//   tokens in query blocks of 64: 609-624 us, 550 TFLOP/s).
+//   long query blocks: the instructions that one wave a SIMD issues, scores, softmax and products in turn
+//   (8192 tokens in query blocks of 64: 606 us, 563 TFLOP/s; counters: VALU 43 % of its time, MFMA 24).
+//   More in flight does not help: two key buffers 663 us against 641 on one card.
 template <int DQK, int DV, int RB, bool SKIP>
 __global__ __attribute__((amdgpu_flat_work_group_size(NTHREADS, NTHREADS), amdgpu_waves_per_eu(RB == 4 || DQK == 192 ? 1 : 2)))
 void attend_kernel(AttendArgs a) {

@@ -58,9 +58,15 @@ class BlockSparseAttention:
         self.tokens = self.num_query_blocks = self.workspace_bytes = self.select_bytes = 0
 
     # -- planning -----------------------------------------------------------
+    def _not_capturing(self, what: str):
+        with torch.cuda.device(self.device):
+            if torch.cuda.is_current_stream_capturing():
+                raise RuntimeError("%s() copies from the host: call it before the capture" % what)
+
     def plan(self, cu_q: Sequence[int], kv_start: Sequence[int], prefix_len: Sequence[int]) -> int:
         """Cut the chunk's segments (as for ``ChunkAttention.plan``; kv_start a multiple of block_size)
-        into query blocks. Returns their number."""
+        into query blocks. Returns their number. Not within a graph capture."""
+        self._not_capturing("plan")
         qb = B.vpp_query_blocks(cu_q, kv_start, prefix_len, self.cfg.query_block, self.cfg.block_size)
         cu = [int(x) for x in cu_q]
         used = [s for s in range(len(kv_start)) if cu[s + 1] > cu[s]]
@@ -89,8 +95,10 @@ class BlockSparseAttention:
 
     def completed(self, cu_q: Sequence[int], kv_start: Sequence[int], prefix_len: Sequence[int], host_block_table,
                   page_size: int) -> torch.Tensor:
-        """The blocks of the cache (int64 indices, on the GPU) that a chunk completes, for ``summarize``;
-        host_block_table is a host copy of the block table (array [segments, pages_per_row])."""
+        """The blocks of the cache (int64 indices, on the GPU, copied there on the current stream) that a
+        chunk completes, for ``summarize``; host_block_table is a host copy of the block table (array
+        [segments, pages_per_row]). Not within a graph capture."""
+        self._not_capturing("completed")
         ids = B.vpp_completed_blocks(cu_q, kv_start, prefix_len, host_block_table, page_size, self.cfg.block_size)
         return torch.from_numpy(ids).pin_memory().to(self.device, non_blocking=True)
 

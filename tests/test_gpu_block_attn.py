@@ -702,3 +702,31 @@ def test_a_captured_layer_step_and_its_replays():
         for b in sets[:2]:
             assert all(torch.equal(x, y) for x, y in zip(b, sets[2]))
         assert bool(sets[2][2].float().abs().sum() > 0)
+
+
+def test_planning_is_refused_within_a_capture():
+    attn = _attn(4, 2, 64, 64, 4)
+    attn.plan([0, 5], [0], [70])
+    q, sums = _bf16(np.random.default_rng(1), 5, 4, 64).to(DEV), attn.new_summaries(2, 64)
+    table = torch.tensor([[1, 0]], dtype=torch.int32, device=DEV)
+    blocks = attn.select(q, sums, table)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        for call in (lambda: attn.plan([0, 5], [0], [70]), lambda: attn.completed([0, 5], [0], [70], [[1, 0]], 64)):
+            with pytest.raises(RuntimeError, match="before the capture"):
+                call()
+        attn.select(q, sums, table, blocks)
+    before = blocks.clone()
+    blocks.fill_(7)
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(blocks, before)
+
+
+def test_a_chunk_that_completes_no_block():
+    attn = _attn(4, 2, 64, 64, 4)
+    done = attn.completed([0, 5], [0], [70], np.array([[1, 0]], dtype=np.int32), 64)
+    assert done.numel() == 0 and done.is_cuda and done.dtype == torch.int64
+    sums = attn.new_summaries(2, 64)
+    attn.summarize(torch.ones(2, 64, 2, 64, dtype=torch.bfloat16, device=DEV), done, sums)
+    assert not sums.any()

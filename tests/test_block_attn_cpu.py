@@ -1,12 +1,17 @@
 """Block-sparse attention on the host (no GPU): query blocks, completed blocks, refusals."""
 import ctypes
 import math
+import os
+import re
+import subprocess
 
 import numpy as np
 import pytest
 
 import sparse_ref as R
+import test_asm_hazards as H
 from paper_2608_26523_amd import binding as B
+from paper_2608_26523_amd import build as BLD
 
 GOOD = 1 << 20  # an aligned address that no refused call reads
 
@@ -197,3 +202,26 @@ def test_reference_grid_and_rotation():
     assert np.allclose(y[0, 0], [0, 0, 1, 0], atol=1e-15)
     y, _ = R.rotated(np.array([[[1.0, 0.0, 2.0, 0.0]]]), [3], [math.pi / 2, 0.0], 0, True, scale=2.0, inverse=True)
     assert np.allclose(y[0, 0], [0, 2, 4, 0], atol=1e-14)
+
+
+def test_scalar_alu_asm_declares_scc():
+    for path in BLD.MORE_SRCS:
+        for template, clobbers in H._asm_statements(open(path).read()):
+            ops = [ln.split()[0] for ln in template.replace("\\n", "\n").replace("\\t", "").splitlines() if ln.strip()]
+            assert "scc" in clobbers or not any(H.SCC_WRITE.match(op) for op in ops), template
+
+
+@pytest.mark.skipif(not os.path.exists(BLD.hipcc()), reason="hipcc not installed")
+def test_device_code_keeps_scc_and_uses_no_scratch(tmp_path):
+    """No SCC value is read across a copy that writes it; and no spill to memory, whose loads the copies' counted
+    waits would take for copies."""
+    out = str(tmp_path / "attn.s")
+    base = [BLD.hipcc()] + [f for f in BLD.HIPCC_FLAGS if f not in ("-shared", "-Wall")] + ["-I", BLD.INCLUDE]
+    src = next(p for p in BLD.MORE_SRCS if p.endswith("vpp_block_attn.hip"))
+    log = subprocess.run(base + ["--cuda-device-only", "-S", "-o", out, src], capture_output=True, text=True, timeout=600)
+    assert log.returncode == 0, log.stderr[-2000:]
+    text = open(out).read()
+    assert "buffer_load_dwordx4" in text and ";;#ASMSTART" in text
+    assert H._scan(text) == []
+    sizes = re.findall(r"\.amdhsa_private_segment_fixed_size (\d+)", text)
+    assert len(sizes) == 14 and set(sizes) == {"0"}

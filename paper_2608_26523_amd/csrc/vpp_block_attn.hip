@@ -83,6 +83,27 @@ __device__ __forceinline__ int vswz(int key, int g) {
     else return g ^ (((key >> 1) & 3) << 1);
 }
 
+// O of 64 columns fills the accumulation registers. In rarely taken branches it is read from there by asm: for
+// ordinary operands the compiler copies all of it out every tile (8192 tokens in query blocks of 64: 606 us,
+// so 563). The asm does not wait for matrix products: products_done() first.
+template <bool ASM>
+__device__ __forceinline__ void products_done() {
+    if constexpr (ASM) asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");
+}
+template <bool ASM>
+__device__ __forceinline__ float out_of_agprs(float x) {
+    if constexpr (ASM) {
+        float y;
+        asm volatile("v_accvgpr_read_b32 %0, %1" : "=v"(y) : "a"(x));
+        return y;
+    }
+    return x;
+}
+template <bool ASM>
+__device__ __forceinline__ f32x4 out_of_agprs(f32x4 x) {
+    return f32x4{out_of_agprs<ASM>(x[0]), out_of_agprs<ASM>(x[1]), out_of_agprs<ASM>(x[2]), out_of_agprs<ASM>(x[3])};
+}
+
 // A listed block, once for all query blocks of a workgroup that list it.
 struct Element {
     int key0, page, row;  // position of its first key; its page and first row of it
@@ -214,8 +235,8 @@ __device__ __forceinline__ int list_elements(const AttendArgs& a, const Entry* e
 //   every token its own list: the blocks that few rows share, out of the caches (4096 tokens of 32/8
 //   heads, 16 blocks each, 14 GB of tiles: 640 us, 22 TB/s);
 //   long query blocks: the instructions that one wave a SIMD issues, scores, softmax and products in turn
-//   (8192 tokens in query blocks of 64: 606 us, 563 TFLOP/s; counters: VALU 43 % of its time, MFMA 24).
-//   More in flight does not help: two key buffers 663 us against 641 on one card.
+//   (8192 tokens in query blocks of 64: 563 us, 606 TFLOP/s). More in flight does not help, nor the next
+//   scores beside this softmax: two key buffers 663 us against 641 on one card, scores ahead 651 to 627.
 template <int DQK, int DV, int RB, bool SKIP>
 __global__ __attribute__((amdgpu_flat_work_group_size(NTHREADS, NTHREADS), amdgpu_waves_per_eu(RB == 4 || DQK == 192 ? 1 : 2)))
 void attend_kernel(AttendArgs a) {
@@ -380,7 +401,7 @@ void attend_kernel(AttendArgs a) {
                 if constexpr (VB == 2) copy_v(next, buf ^ 1);
             }
             const bool masked = now.key0 + BT - 1 > first_pos, partial = now.mask != all_bits;
-            if (masked || partial) {
+            if (__builtin_expect(masked || partial, SKIP)) {
 #pragma unroll
                 for (int rb = 0; rb < RB; ++rb) {
                     if (SKIP && !(now.mask & bits[rb])) continue;
@@ -402,7 +423,8 @@ void attend_kernel(AttendArgs a) {
                                 fmaxf(fmaxf(s[rb][1][0], s[rb][1][1]), fmaxf(s[rb][1][2], s[rb][1][3]))) * a.scale_log2;
                 above = above || top[rb] > m_run[rb] + LAZY;
             }
-            if (__ballot(above)) {
+            if (__builtin_expect(__ballot(above) != 0, 0)) {
+                products_done<RB == 4>();
 #pragma unroll
                 for (int rb = 0; rb < RB; ++rb) {
                     const float m = fmaxf(m_run[rb], max_xor32(max_xor16(top[rb])));
@@ -410,7 +432,7 @@ void attend_kernel(AttendArgs a) {
                     m_run[rb] = m;
                     l_run[rb] *= alpha;
 #pragma unroll
-                    for (int d = 0; d < DB; ++d) o[rb][d] *= alpha;
+                    for (int d = 0; d < DB; ++d) o[rb][d] = out_of_agprs<RB == 4>(o[rb][d]) * alpha;
                 }
             }
             bf16x8 p[RB];
@@ -431,7 +453,7 @@ void attend_kernel(AttendArgs a) {
             if (more) asm volatile("s_waitcnt vmcnt(%0)" ::"i"(K_LOADS + (VB == 2 ? V_LOADS : 0)) : "memory");
             else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
             bool wild = false;
-            if (careful && (masked || partial)) {
+            if (__builtin_expect(careful && (masked || partial), 0)) {
                 // values that are not finite count as 0 here; the rows that see them get them after the product
 #pragma unroll 1
                 for (int i = 0; i < V_LOADS; ++i) {
@@ -460,7 +482,8 @@ void attend_kernel(AttendArgs a) {
                 for (int rb = 0; rb < RB; ++rb)
                     if (!SKIP || now.mask & bits[rb]) o[rb][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, p[rb], o[rb][d], 0, 0, 0);
             }
-            if (wild) {
+            if (__builtin_expect(wild, 0)) {
+                products_done<RB == 4>();
                 const u16* const v0 = vbase + now.page * a.v_sp + (int64_t)now.row * a.v_st + grp * 4;
 #pragma unroll 1
                 for (int key = 0; key < now.n; ++key)
@@ -472,7 +495,7 @@ void attend_kernel(AttendArgs a) {
                             const float v = __uint_as_float(i % 2 ? x[i / 2] & 0xffff0000u : x[i / 2] << 16);
 #pragma unroll
                             for (int rb = 0; rb < RB; ++rb)
-                                if (!(fabsf(v) < INFINITY) && now.key0 + key <= (now.mask & bit[rb] ? lim[rb] : -1)) o[rb][d][i] += v;
+                                if (!(fabsf(v) < INFINITY) && now.key0 + key <= (now.mask & bit[rb] ? lim[rb] : -1)) o[rb][d][i] = out_of_agprs<RB == 4>(o[rb][d][i]) + v;
                         }
                     }
             }

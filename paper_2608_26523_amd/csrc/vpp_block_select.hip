@@ -261,13 +261,13 @@ __global__ __launch_bounds__(64 * (NW == 1 ? LISTS : NW)) void list_kernel(Selec
 // in registers as A operands, on their grid; the waves share the blocks, whose summaries come
 // straight from memory as B operands, NT tiles ahead. Rows of a query block start on a power of two
 // up to 16 or a multiple of 16, and those past its last repeat it. RM: rows of a query block, 1
-// (one or two), 4 (or 8), 16, 32 (or more). WHOLE: one query block a workgroup, its scores go to LDS, and
+// (one or two), 4 (or 8), 16, 32, 64, 128 (with eight tiles), 48 (any other above 16, or 128 with four). WHOLE: one query block a workgroup, its scores go to LDS, and
 // the workgroup makes its list.
 // Products of two 8-bit grids are whole multiples of a step and their sums stay below 2^24 of them, so fp32
 // holds every sum exactly, whatever the order: lists do not depend on tiles, splits or slabs.
 // Bound by the matrix unit and, one or two waves a SIMD, by what runs beside it: maxima, and moves of scalars
-// that do not fit the registers. 16384 rows in query blocks of 64, 16 heads, dqk 192, behind 508K: 1313
-// us, 618 TFLOP/s; 4096 tokens of 32/8 heads behind 28672, a list each: 73 us.
+// that do not fit the registers. 16384 rows in query blocks of 64, 16 heads, dqk 192, behind 508K: 1.2
+// ms, 674 TFLOP/s; 4096 tokens of 32/8 heads behind 28672, a list each: 73 us.
 constexpr int WHOLE_BLOCKS = 2048;
 template <int DQK, int MT, int NT, int RM, bool WHOLE>
 __global__ __launch_bounds__(NTHREADS) void score_kernel(SelectArgs a) {
@@ -396,7 +396,19 @@ __global__ __launch_bounds__(NTHREADS) void score_kernel(SelectArgs a) {
                         const float x = both(both(v[m], v[m + 1], swap16), both(v[m + 2], v[m + 3], swap16), swap32);
                         if (entry[m] >= 0) put(entry[m], block, x);
                     }
-                } else if constexpr (RM == 32) {
+                } else if constexpr (RM > 16 && RM != 48) {
+                    // RM / 16 tiles, which are always of one pass: no branch on their number beside the products
+                    // (16384 rows in query blocks of 64: 1341 us with the one below, so 1291)
+                    constexpr int per = RM / 16;
+#pragma unroll
+                    for (int m = 0; m < MT; m += per) {
+                        float x = v[m];
+#pragma unroll
+                        for (int i = 1; i < per; ++i) x = max_finite(x, v[m + i]);
+                        x = max_xor32<true>(max_xor16<true>(x));
+                        if (grp == 0 && entry[m] >= 0) put(entry[m], block, x);
+                    }
+                } else if constexpr (RM == 48) {
                     // several tiles to a query block; what its earlier ones left in memory counts (only the lane
                     // whose block it is reads and writes it: the waves are not at the same tiles)
                     const int per = a.rows / 16;
@@ -435,7 +447,7 @@ __global__ __launch_bounds__(NTHREADS) void score_kernel(SelectArgs a) {
 #pragma unroll
                     for (int m = 0; m < MT; ++m) now[m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(qf[m][s], k[s], now[m], 0, 0, 0);
                 if (then_block >= 0) take(then, then_block);
-                if constexpr (PACKED || RM == 32) {
+                if constexpr (PACKED || RM > 16) {
 #pragma unroll
                     for (int i = 0; i < KS * MT; ++i) {  // a product, then 2 of the maxima's operations
                         __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
@@ -458,8 +470,8 @@ __global__ __launch_bounds__(NTHREADS) void score_kernel(SelectArgs a) {
                 for (int n = 0; n < NT; ++n) {
                     const int now = (d0 + n) % 2;
                     tile(kf[buf][n], d[now], d[1 - now], block[1 - now]);
-                    // past the last: its score again, the same (but RM = 32, which leaves them out)
-                    block[now] = RM == 32 ? b + n * 16 : min(b + n * 16, hi - 1);
+                    // past the last: its score again, the same (but RM = 48, which leaves them out)
+                    block[now] = RM == 48 ? b + n * 16 : min(b + n * 16, hi - 1);
                     __builtin_amdgcn_sched_barrier(0);
                 }
             };
@@ -574,10 +586,10 @@ extern "C" vpp_status_t vpp_block_summarize_paged(const vpp_block_attn_config_t*
 namespace {
 template <int DQK, int RM>
 auto pick_rows(int mt) {  // 0: the whole selection
-    auto* four = score_kernel<DQK, 4, 1, RM, false>;
+    auto* four = score_kernel<DQK, 4, 1, RM <= 64 ? RM : 48, false>;
     if constexpr (DQK == 192)
         if (mt == 8) return score_kernel<DQK, 8, 1, RM, false>;
-    if constexpr (RM != 32) {  // more rows than a tile has: never one tile
+    if constexpr (RM <= 16) {  // more rows than a tile has: never one tile
         if (mt == 1) return score_kernel<DQK, 1, 4, RM, false>;
         if (mt == 0) return score_kernel<DQK, 1, 4, RM, true>;
     }
@@ -585,7 +597,9 @@ auto pick_rows(int mt) {  // 0: the whole selection
 }
 template <int DQK>
 auto pick_score(int mt, int rows) {
-    return rows < 4 ? pick_rows<DQK, 1>(mt) : rows < 16 ? pick_rows<DQK, 4>(mt) : rows == 16 ? pick_rows<DQK, 16>(mt) : pick_rows<DQK, 32>(mt);
+    return rows < 4 ? pick_rows<DQK, 1>(mt) : rows < 16 ? pick_rows<DQK, 4>(mt) : rows == 16 ? pick_rows<DQK, 16>(mt)
+           : rows == 32 ? pick_rows<DQK, 32>(mt) : rows == 64 ? pick_rows<DQK, 64>(mt)
+           : rows == 128 && mt == 8 ? pick_rows<DQK, 128>(mt) : pick_rows<DQK, 48>(mt);
 }
 
 // Blocks that the scores of a chunk up to max_kv_len have room for, and the query blocks of a slab.

@@ -185,10 +185,11 @@ def test_selection_of_many_query_blocks(heads, size, tokens):
     assert np.array_equal(got.cpu().numpy(), want)
 
 
-@pytest.mark.parametrize("heads,size", [((32, 1, 64, 64), 16), ((16, 2, 192, 128), 64), ((24, 2, 128, 128), 32)])
+@pytest.mark.parametrize("heads,size", [((32, 1, 64, 64), 16), ((16, 2, 192, 128), 64), ((24, 2, 128, 128), 32),
+                                        ((8, 4, 192, 128), 64)])
 @pytest.mark.parametrize("prefix", [2500, 4200])
 def test_selection_of_query_blocks_of_many_rows(heads, size, prefix):
-    """384 to 512 rows a query block, taken in several passes whose maxima meet in memory; half of the blocks
+    """128 to 512 rows a query block, those above 128 in several passes whose maxima meet in memory; half of the blocks
     are chosen, so that the last one's score decides too."""
     hq, hkv, d, dv = heads
     rng = np.random.default_rng(prefix + size)
